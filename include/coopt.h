@@ -52,7 +52,8 @@ typedef enum {
   COOPT_ERR_UNSUPPORTED = -2, /* shape outside the compiled set (see each call)          */
   COOPT_ERR_WORKSPACE = -3,   /* workspace missing or smaller than coopt_workspace_bytes */
   COOPT_ERR_CUDA = -4,        /* a CUDA runtime call or the launch failed                */
-  COOPT_ERR_TIMEOUT = -5      /* device side: a bounded wait ran out (workspace word 0)  */
+  COOPT_ERR_TIMEOUT = -5,     /* device side: a bounded wait ran out (workspace word 0)  */
+  COOPT_ERR_PAGES = -6        /* device side: the pool has too few free blocks (workspace word 0) */
 } coopt_status;
 
 /* COOPT_KV_FP8_E5M2 is an ablation of the FP8 format, which Section 3.1 leaves open: the same granule layout and the
@@ -309,6 +310,91 @@ int coopt_step_staging_layout(int32_t batch, int32_t num_q_heads, int32_t num_kv
 int coopt_decode_step_host(const coopt_cache* cache, const void* step_inputs_host, void* out_host, int32_t max_blocks_per_seq,
                            int32_t batch, int32_t num_q_heads, float sm_scale, void* staging, size_t staging_bytes, void* plan,
                            size_t plan_bytes, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Attention with a sliding window and sinks: the query at position t of a sequence sees the positions j <= t with
+ * j > t - window (the last `window` tokens, itself among them) or j < sinks (the sequence's first tokens, which stay visible).
+ * Softmax, scales and grouping are those of coopt_paged_decode.  Only blocks that hold a visible token of some query of the
+ * sequence are read, and only their table entries: what lies between the sinks and the window may have been released
+ * (coopt_pages_release) and hold any entry.  A window that reaches back to the sequence's start gives coopt_paged_decode's
+ * (coopt_paged_chunked's causal) result.
+ *   window >= 1, sinks >= 0; either may exceed the contexts.
+ *
+ * coopt_window_decode -- one query token per sequence, at position context_lens[b] - 1; the arguments of coopt_paged_decode.
+ *   k_new, v_new, slot_mapping  the step's new tokens, written first, as for coopt_decode_step_planned (the same precondition:
+ *                               the new token of sequence b is its last position; FP8 caches take them in the same launch, a
+ *                               bf16 cache by coopt_kv_write's rule in a launch of its own); all three NULL = none
+ *   context_lens                counting the new token; 0 gives an all-zero output row
+ * coopt_window_prefill -- runs of query tokens; the arguments of coopt_paged_chunked without chunks, always causal.
+ *   cu_q_lens                   runs may have any length, 0 and 1 included; total_q = cu_q_lens[batch] sizes the launch, and rows
+ *                               of q and out from cu_q_lens[batch] on are left alone.  Rows that see nothing (a run longer
+ *                               than its context) are zero.
+ *   workspace                   >= the control words (any workspace that coopt_workspace_init has prepared)
+ * Errors: as coopt_paged_decode, plus INVALID_ARG (window, sinks), UNSUPPORTED (max_blocks_per_seq > 2^25; a bf16 cache in
+ * coopt_window_prefill).  Both FP8 formats at both head dims.
+ */
+int coopt_window_decode(const coopt_cache* cache, const void* k_new, const void* v_new, int64_t kv_token_stride,
+                        const int64_t* slot_mapping, const void* q, void* out, const int32_t* block_table,
+                        int32_t max_blocks_per_seq, const int32_t* context_lens, int32_t batch, int32_t num_q_heads,
+                        int32_t window, int32_t sinks, float sm_scale, void* workspace, size_t workspace_bytes, void* stream);
+int coopt_window_prefill(const coopt_cache* cache, const void* q, void* out, const int32_t* cu_q_lens, const int32_t* block_table,
+                         int32_t max_blocks_per_seq, const int32_t* context_lens, int32_t batch, int32_t num_q_heads,
+                         int32_t total_q, int32_t window, int32_t sinks, float sm_scale, void* workspace, size_t workspace_bytes,
+                         void* stream);
+
+/*
+ * Pages: the physical blocks of a cache handed out, shared, copied and taken back on the device, for all layers that share a
+ * block table.  A pool is three DEVICE arrays of the caller's:
+ *   refs          int32 [num_blocks]: how many table entries (or other holders) hold the block; 0 or less = free
+ *   block_table   int32 [rows][max_blocks_per_seq], as the attention calls read it (row b is sequence b); -1 = no block
+ *   context_lens  int32 [rows]; 0 = the row is unused
+ * A new pool has all refs 0, all entries -1, all lengths 0.  Blocks are handed out lowest first, in the order of the call's
+ * list, so results depend on the inputs alone.  Calls on one pool (and the attention calls that read its table) are ordered
+ * by the stream.
+ *   caches        HOST array of num_caches descriptors, the layers, all of one shape and of the pool's num_blocks
+ *   workspace     DEVICE, >= coopt_pages_workspace_bytes(num_blocks, rows), prepared once by coopt_workspace_init; its first
+ *                 int32 reports what went wrong on the device, as everywhere: COOPT_ERR_INVALID_ARG (a row, length, entry or
+ *                 list as described below) or COOPT_ERR_PAGES (too few free blocks).  What is refused on the device is left as
+ *                 it was; the rest of the call is carried out.
+ *
+ * coopt_pages_copy -- block src[i] copied over block dst[i] in every layer.  Pairs with an id out of range are ignored.
+ *   Precondition: no block is the destination of two pairs, or of one and the source of another.
+ * coopt_pages_reserve -- row row_ids[i] gets blocks for new_lens[i] tokens: entries without a block between its length and the
+ *   new one get one each, refs 1, and its length becomes new_lens[i].  A row is served if the free blocks suffice for it and
+ *   the rows before it in the list.  Refused: rows out of range, a row's second mention, lengths that shrink or exceed the table.
+ * coopt_pages_fork -- row children[i] becomes a copy of row parents[i]: full blocks are shared (refs + 1), a last block that is
+ *   partly filled is copied to a new one in every layer (both may be appended to from then on), released entries stay
+ *   released, blocks reserved past the parent's length are not taken over.  Refused: rows out of range, a child whose length is not 0, a
+ *   child's second mention, a parent that is a child in the same call.  num_caches 0: table and counts only.
+ * coopt_pages_release -- window 0: every block of row row_ids[i] is given back (refs - 1), its entries become -1 and its length
+ *   0.  window > 0: the blocks that neither hold one of the first `sinks` tokens nor one of the last `window` ones are given
+ *   back, as coopt_window_decode at this length, and any later one, does not read them.  A row named twice is released once.
+ * coopt_pages_compact -- the U blocks in use (refs > 0) become the blocks 0 .. U-1: those numbered U and above are copied, in
+ *   order, into the free ones below, in every layer.  table_out and refs_out (the pool's own arrays, or others of their size)
+ *   get the renumbered table and counts, used_out (DEVICE int32) gets U.  Entries that name a free block, or none of the pool,
+ *   become -1 and are reported.  Contents of the blocks from U on are left as they were.
+ * Errors: INVALID_ARG, UNSUPPORTED (more than 2^20 blocks, 8192 rows or 2^25 blocks a row; 2^31 pairs or blocks times kv heads),
+ * WORKSPACE, CUDA.  Every argument is checked before anything is launched.
+ */
+typedef struct coopt_pages {
+  int32_t* refs;
+  int32_t* block_table;
+  int32_t* context_lens;
+  int32_t num_blocks;
+  int32_t rows;
+  int32_t max_blocks_per_seq;
+} coopt_pages;
+
+size_t coopt_pages_workspace_bytes(int32_t num_blocks, int32_t rows);
+int coopt_pages_copy(const coopt_cache* caches, int32_t num_caches, const int32_t* src, const int32_t* dst, int32_t num_pairs, void* stream);
+int coopt_pages_reserve(const coopt_pages* pages, const int32_t* row_ids, const int32_t* new_lens, int32_t num_rows, void* workspace,
+                        size_t workspace_bytes, void* stream);
+int coopt_pages_fork(const coopt_cache* caches, int32_t num_caches, const coopt_pages* pages, const int32_t* parents, const int32_t* children,
+                     int32_t num_forks, void* workspace, size_t workspace_bytes, void* stream);
+int coopt_pages_release(const coopt_pages* pages, const int32_t* row_ids, int32_t num_rows, int32_t window, int32_t sinks, void* workspace,
+                        size_t workspace_bytes, void* stream);
+int coopt_pages_compact(const coopt_cache* caches, int32_t num_caches, const coopt_pages* pages, int32_t* table_out, int32_t* refs_out, int32_t* used_out,
+                        void* workspace, size_t workspace_bytes, void* stream);
 
 /* Workspace size for a call with these arguments (chunk_size = 0 for coopt_paged_decode).
  * Host arithmetic only (it asks the current device for its SM count once). */

@@ -140,3 +140,45 @@ def paged_attention_chunked(q: np.ndarray, kv: np.ndarray, block_table: np.ndarr
                 partials[(b, h)] = (m, l, o)
                 out[b, h] = merge_partials(m, l, o)
     return out, partials
+
+
+def window_attention(q: np.ndarray, kv, block_table: np.ndarray, context_lens, window: int, sinks: int, cu_q_lens=None,
+                     sm_scale: float | None = None):
+    """Attention with a sliding window and sinks, float64: the query at position t sees the positions j <= t (inside the
+    context) with j > t - window or j < sinks; nothing visible gives zeros.  The n query rows of a sequence are its last n
+    positions.  Table entries of blocks without a visible token are not looked at.
+
+    Returns ``(out, spread)`` [total_q, Hq, D]; ``spread`` is sum_j p_j |v_j|, what errors of the weights are measured by.
+    """
+    total_q, num_q_heads, head_dim = q.shape
+    num_kv_heads = (kv[0] if isinstance(kv, tuple) else kv).shape[1]
+    group = num_q_heads // num_kv_heads
+    if cu_q_lens is None:
+        cu_q_lens = np.arange(len(context_lens) + 1)
+    if sm_scale is None:
+        sm_scale = 1.0 / np.sqrt(head_dim)
+    out, spread = np.zeros((total_q, num_q_heads, head_dim)), np.zeros((total_q, num_q_heads, head_dim))
+    for b, length in enumerate(context_lens):
+        length, r0, r1 = int(length), int(cu_q_lens[b]), int(cu_q_lens[b + 1])
+        t = length - (r1 - r0) + np.arange(r1 - r0)
+        j = np.arange(length)
+        seen = (j[None] <= t[:, None]) & ((j[None] > t[:, None] - window) | (j[None] < sinks))
+        some = np.nonzero(seen.any(axis=0))[0]                          # positions that some query sees
+        if some.size == 0:
+            continue
+        blocks = some // BLOCK_SIZE
+        compact = np.unique(blocks)
+        row = np.asarray(block_table[b])[compact]                       # a table of those blocks alone
+        at = np.searchsorted(compact, blocks) * BLOCK_SIZE + some % BLOCK_SIZE
+        for g in range(num_kv_heads):
+            K, V = gather_kv(kv, row, compact.size * BLOCK_SIZE, g)
+            K, V = K[at], V[at]
+            for h in range(g * group, (g + 1) * group):
+                s = (q[r0:r1, h].astype(np.float64) @ K.T) * sm_scale
+                s = np.where(seen[:, some], s, -np.inf)
+                top = s.max(axis=1, keepdims=True)
+                p = np.exp(s - np.where(np.isfinite(top), top, 0.0))
+                total = p.sum(axis=1, keepdims=True)
+                p = p / np.where(total > 0, total, 1.0)
+                out[r0:r1, h], spread[r0:r1, h] = p @ V, p @ np.abs(V)
+    return out, spread

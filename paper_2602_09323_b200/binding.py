@@ -43,6 +43,11 @@ class coopt_layer_io(ctypes.Structure):
                 ("slot_mapping", ctypes.c_void_p), ("q", ctypes.c_void_p), ("out", ctypes.c_void_p)]
 
 
+class coopt_pages(ctypes.Structure):
+    _fields_ = [("refs", ctypes.c_void_p), ("block_table", ctypes.c_void_p), ("context_lens", ctypes.c_void_p), ("num_blocks", ctypes.c_int32),
+                ("rows", ctypes.c_int32), ("max_blocks_per_seq", ctypes.c_int32)]
+
+
 FLAG_OVERLAP_PREVIOUS = 1
 
 _SIGNATURES = {
@@ -90,6 +95,24 @@ _SIGNATURES = {
     "coopt_selftest_layers_launch": (ctypes.c_int, [ctypes.POINTER(coopt_layer_io), ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p,
                                                     ctypes.c_int32, ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32, ctypes.c_size_t,
                                                     ctypes.c_uint32, ctypes.c_void_p, ctypes.c_void_p]),
+    "coopt_window_decode": (ctypes.c_int, [ctypes.POINTER(coopt_cache), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                           ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p, ctypes.c_int32,
+                                           ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_float, ctypes.c_void_p, ctypes.c_size_t,
+                                           ctypes.c_void_p]),
+    "coopt_window_prefill": (ctypes.c_int, [ctypes.POINTER(coopt_cache), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                            ctypes.c_int32, ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
+                                            ctypes.c_int32, ctypes.c_float, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "coopt_pages_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int32] * 2),
+    "coopt_pages_copy": (ctypes.c_int, [ctypes.POINTER(coopt_cache), ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32,
+                                        ctypes.c_void_p]),
+    "coopt_pages_reserve": (ctypes.c_int, [ctypes.POINTER(coopt_pages), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p,
+                                           ctypes.c_size_t, ctypes.c_void_p]),
+    "coopt_pages_fork": (ctypes.c_int, [ctypes.POINTER(coopt_cache), ctypes.c_int32, ctypes.POINTER(coopt_pages), ctypes.c_void_p,
+                                        ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "coopt_pages_release": (ctypes.c_int, [ctypes.POINTER(coopt_pages), ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
+                                           ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "coopt_pages_compact": (ctypes.c_int, [ctypes.POINTER(coopt_cache), ctypes.c_int32, ctypes.POINTER(coopt_pages), ctypes.c_void_p,
+                                           ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
     "coopt_selftest_bounded_wait": (ctypes.c_int, [ctypes.c_uint64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]),
     "coopt_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "coopt_version": (ctypes.c_int, []),
@@ -146,15 +169,18 @@ else:
 
 
 class Cache:
-    """A paged KV cache in device memory plus the C descriptor that names it."""
+    """A paged KV cache in device memory plus the C descriptor that names it.  ``data``: memory of the caller's that holds
+    (or will hold) it, a contiguous uint8 CUDA tensor of coopt_cache_bytes; else zeroed memory is allocated."""
 
     def __init__(self, num_blocks: int, num_kv_heads: int, head_dim: int, dtype: int = KV_FP8_E4M3,
-                 device: str = "cuda"):
+                 device: str = "cuda", data: Optional[torch.Tensor] = None):
         lib = load_library()
         nbytes = lib.coopt_cache_bytes(num_blocks, num_kv_heads, head_dim, dtype)
         if nbytes == 0:
             raise CooptError(-2, "coopt_cache_bytes")
-        self.data = torch.zeros(nbytes, dtype=torch.uint8, device=device)
+        if data is not None and (data.dtype is not torch.uint8 or not data.is_contiguous() or data.numel() != nbytes):
+            raise ValueError(f"a cache of this shape is {nbytes} contiguous bytes")
+        self.data = torch.zeros(nbytes, dtype=torch.uint8, device=device) if data is None else data
         self.num_blocks, self.num_kv_heads, self.head_dim, self.dtype = num_blocks, num_kv_heads, head_dim, dtype
         self.granule_bytes = lib.coopt_granule_bytes(head_dim, dtype)
         self.desc = coopt_cache(self.data.data_ptr(), num_blocks, num_kv_heads, head_dim, BLOCK_SIZE, dtype)
@@ -383,3 +409,173 @@ def decode_step_host(cache: Cache, step_inputs: torch.Tensor, out: torch.Tensor,
                                                num_q_heads, float(sm_scale), staging.data_ptr(), staging.numel(), plan.data_ptr(),
                                                plan.numel(), workspace.data_ptr(), workspace.numel(), _stream())
     _check(st, "coopt_decode_step_host")
+
+
+# ---- attention with a sliding window and sinks -------------------------------------------------------------------
+# The calls of this part and the next say what they do not take by ValueError, also under ``python -O``.
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _here(*tensors) -> None:
+    """Tensors of the current device, on which the call is enqueued."""
+    device = torch.cuda.current_device() if _current_device is None else _current_device()
+    for t in tensors:
+        _need(t.is_cuda and t.get_device() == device, "every tensor has to be on the current CUDA device")
+
+
+def _window_inputs(cache: Cache, q, block_table, context_lens, workspace, out):
+    _here(cache.data, q, block_table, context_lens, workspace, out)
+    _need(q.dtype is _BF16 and q.is_contiguous() and q.dim() == 3 and q.shape[2] == cache.head_dim, "q: contiguous bf16 [rows, heads, head_dim]")
+    _need(out.dtype is _BF16 and out.is_contiguous() and out.shape == q.shape, "out: like q")
+    _need(block_table.dtype is _I32 and block_table.is_contiguous() and block_table.dim() == 2, "block_table: contiguous int32 [batch, width]")
+    _need(context_lens.dtype is _I32 and context_lens.is_contiguous() and context_lens.numel() == block_table.shape[0],
+          "context_lens: contiguous int32, one per row of the table")
+
+
+def window_decode(cache: Cache, q: torch.Tensor, block_table: torch.Tensor, context_lens: torch.Tensor, window: int, sinks: int,
+                  sm_scale: float, workspace: torch.Tensor, k_new: Optional[torch.Tensor] = None, v_new: Optional[torch.Tensor] = None,
+                  slot_mapping: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """coopt_window_decode: q bf16 [B, Hq, D] sees the last ``window`` tokens and the first ``sinks``; with k_new, v_new
+    (bf16 [B, Hkv, D], token stride taken from the tensor) and slot_mapping (int64 [B]) the new tokens are written first."""
+    if out is None:
+        out = torch.empty_like(q)
+    _window_inputs(cache, q, block_table, context_lens, workspace, out)
+    _need(q.shape[0] == block_table.shape[0], "one query row per row of the table")
+    stride, new = 0, (None, None, None)
+    if k_new is not None or v_new is not None or slot_mapping is not None:
+        _need(k_new is not None and v_new is not None and slot_mapping is not None, "k_new, v_new and slot_mapping go together")
+        _here(k_new, v_new, slot_mapping)
+        shape = (q.shape[0], cache.num_kv_heads, cache.head_dim)
+        _need(k_new.dtype is _BF16 and v_new.dtype is _BF16 and k_new.shape == shape and v_new.shape == shape, "k_new, v_new: bf16 [B, Hkv, D]")
+        at = k_new.stride()
+        _need(at == v_new.stride() and at[2] == 1 and (at[1] == shape[2] or shape[1] == 1), "k_new, v_new: the same strides, heads and dims dense")
+        _need(slot_mapping.dtype is _I64 and slot_mapping.is_contiguous() and slot_mapping.numel() == shape[0], "slot_mapping: contiguous int64 [B]")
+        stride = at[0] if shape[0] > 1 else shape[1] * shape[2]
+        new = (k_new.data_ptr(), v_new.data_ptr(), slot_mapping.data_ptr())
+    st = load_library().coopt_window_decode(cache.ref(), new[0], new[1], stride, new[2], q.data_ptr(), out.data_ptr(), block_table.data_ptr(),
+                                            block_table.shape[1], context_lens.data_ptr(), q.shape[0], q.shape[1], int(window), int(sinks),
+                                            float(sm_scale), workspace.data_ptr(), workspace.numel(), _stream())
+    _check(st, "coopt_window_decode")
+    return out
+
+
+def window_prefill(cache: Cache, q: torch.Tensor, cu_q_lens: torch.Tensor, block_table: torch.Tensor, context_lens: torch.Tensor, window: int,
+                   sinks: int, sm_scale: float, workspace: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """coopt_window_prefill: q bf16 [total_q, Hq, D], every query sees the last ``window`` tokens up to itself and the first
+    ``sinks``; cu_q_lens int32 [B + 1] on the device.  Rows from cu_q_lens[B] on are left as they are."""
+    if out is None:
+        out = torch.empty_like(q)
+    _window_inputs(cache, q, block_table, context_lens, workspace, out)
+    _here(cu_q_lens)
+    _need(cu_q_lens.dtype is _I32 and cu_q_lens.is_contiguous() and cu_q_lens.numel() == block_table.shape[0] + 1, "cu_q_lens: contiguous int32 [B + 1]")
+    st = load_library().coopt_window_prefill(cache.ref(), q.data_ptr(), out.data_ptr(), cu_q_lens.data_ptr(), block_table.data_ptr(),
+                                             block_table.shape[1], context_lens.data_ptr(), block_table.shape[0], q.shape[1], q.shape[0],
+                                             int(window), int(sinks), float(sm_scale), workspace.data_ptr(), workspace.numel(), _stream())
+    _check(st, "coopt_window_prefill")
+    return out
+
+
+# ---- pages ---------------------------------------------------------------------------------------------------------
+
+class CacheSet:
+    """The host array of the descriptors of a model's layers, built once (it only holds pointers)."""
+
+    def __init__(self, caches):
+        self.keep = list(caches)
+        self.array = (coopt_cache * len(self.keep))(*[c.desc for c in self.keep])
+
+
+class Pages:
+    """A pool: int32 tensors refs [num_blocks], block_table [rows, width] (-1: no block) and context_lens [rows]."""
+
+    def __init__(self, refs: torch.Tensor, block_table: torch.Tensor, context_lens: torch.Tensor):
+        for t, dims in ((refs, 1), (block_table, 2), (context_lens, 1)):
+            _need(t.dtype is _I32 and t.is_contiguous() and t.dim() == dims, "refs, block_table, context_lens: contiguous int32 [blocks], [rows, width], [rows]")
+        _need(context_lens.shape[0] == block_table.shape[0], "context_lens: one per row of the table")
+        self.refs, self.block_table, self.context_lens = refs, block_table, context_lens
+        rows, width = block_table.shape
+        self.desc = coopt_pages(refs.data_ptr(), block_table.data_ptr(), context_lens.data_ptr(), refs.shape[0], rows, width)
+        self._ref = ctypes.byref(self.desc)
+
+    @classmethod
+    def empty(cls, num_blocks: int, rows: int, max_blocks_per_seq: int, device: str = "cuda") -> "Pages":
+        """A new pool: every block free, every row unused."""
+        return cls(torch.zeros(num_blocks, dtype=_I32, device=device), torch.full((rows, max_blocks_per_seq), -1, dtype=_I32, device=device),
+                   torch.zeros(rows, dtype=_I32, device=device))
+
+    def ref(self):
+        return self._ref
+
+
+def new_pages_workspace(num_blocks: int, rows: int, device: str = "cuda") -> torch.Tensor:
+    """Allocate (torch) and initialise a workspace for the page calls of such a pool."""
+    n = load_library().coopt_pages_workspace_bytes(num_blocks, rows)
+    if n == 0:
+        raise CooptError(-1, "coopt_pages_workspace_bytes")
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    workspace_init(ws)
+    return ws
+
+
+def _lists(*lists) -> None:
+    _here(*lists)
+    for t in lists:
+        _need(t.dtype is _I32 and t.is_contiguous() and t.dim() == 1 and t.shape == lists[0].shape, "lists of rows, lengths or blocks: contiguous int32 of one length")
+
+
+def pages_copy(caches: CacheSet, src: torch.Tensor, dst: torch.Tensor) -> None:
+    """coopt_pages_copy: block src[i] copied over block dst[i] in every layer."""
+    _here(*(c.data for c in caches.keep))
+    _lists(src, dst)
+    st = load_library().coopt_pages_copy(caches.array, len(caches.keep), src.data_ptr(), dst.data_ptr(), src.shape[0], _stream())
+    _check(st, "coopt_pages_copy")
+
+
+def pages_reserve(pages: Pages, row_ids: torch.Tensor, new_lens: torch.Tensor, workspace: torch.Tensor) -> None:
+    """coopt_pages_reserve: row row_ids[i] gets blocks for new_lens[i] tokens, which becomes its length."""
+    _lists(row_ids, new_lens)
+    _here(pages.refs, workspace)
+    st = load_library().coopt_pages_reserve(pages.ref(), row_ids.data_ptr(), new_lens.data_ptr(), row_ids.shape[0], workspace.data_ptr(),
+                                            workspace.numel(), _stream())
+    _check(st, "coopt_pages_reserve")
+
+
+def pages_fork(caches: CacheSet, pages: Pages, parents: torch.Tensor, children: torch.Tensor, workspace: torch.Tensor) -> None:
+    """coopt_pages_fork: row children[i] becomes a copy of row parents[i] that shares its full blocks."""
+    _here(*(c.data for c in caches.keep))
+    _lists(parents, children)
+    _here(pages.refs, workspace)
+    st = load_library().coopt_pages_fork(caches.array, len(caches.keep), pages.ref(), parents.data_ptr(), children.data_ptr(), parents.shape[0],
+                                         workspace.data_ptr(), workspace.numel(), _stream())
+    _check(st, "coopt_pages_fork")
+
+
+def pages_release(pages: Pages, row_ids: torch.Tensor, workspace: torch.Tensor, window: int = 0, sinks: int = 0) -> None:
+    """coopt_pages_release: the rows' blocks are given back, all of them, or (window > 0) those outside window and sinks."""
+    _lists(row_ids)
+    _here(pages.refs, workspace)
+    st = load_library().coopt_pages_release(pages.ref(), row_ids.data_ptr(), row_ids.shape[0], int(window), int(sinks), workspace.data_ptr(),
+                                            workspace.numel(), _stream())
+    _check(st, "coopt_pages_release")
+
+
+def pages_compact(caches: CacheSet, pages: Pages, workspace: torch.Tensor, table_out: Optional[torch.Tensor] = None,
+                  refs_out: Optional[torch.Tensor] = None, used_out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """coopt_pages_compact: the blocks in use become the first ones of the pool; renumbered table and counts into table_out and
+    refs_out (default: in place).  Returns the number of used blocks, an int32 tensor of one element."""
+    table_out = pages.block_table if table_out is None else table_out
+    refs_out = pages.refs if refs_out is None else refs_out
+    if used_out is None:
+        used_out = torch.empty(1, dtype=_I32, device=pages.refs.device)
+    _here(*(c.data for c in caches.keep))
+    _here(pages.refs, workspace, table_out, refs_out, used_out)
+    for t, like in ((table_out, pages.block_table), (refs_out, pages.refs)):
+        _need(t.dtype is _I32 and t.is_contiguous() and t.shape == like.shape, "table_out, refs_out: like the pool's own")
+    _need(used_out.dtype is _I32 and used_out.numel() == 1, "used_out: one int32")
+    st = load_library().coopt_pages_compact(caches.array, len(caches.keep), pages.ref(), table_out.data_ptr(), refs_out.data_ptr(), used_out.data_ptr(),
+                                            workspace.data_ptr(), workspace.numel(), _stream())
+    _check(st, "coopt_pages_compact")
+    return used_out

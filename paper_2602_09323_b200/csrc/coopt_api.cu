@@ -12,8 +12,8 @@ int launch_kv_write(const coopt_cache* c, const void* k, const void* v, int64_t 
                     int num_tokens, cudaStream_t stream);
 int launch_paged_prefill(const coopt_cache* c, const void* q, void* out, const int32_t* cu_q_lens,
                          const int32_t* block_table, int32_t max_blocks_per_seq, const int32_t* context_lens,
-                         int32_t batch, int32_t num_q_heads, int32_t total_q, int32_t causal, float sm_scale,
-                         void* workspace, int num_sms, cudaStream_t stream);
+                         int32_t batch, int32_t num_q_heads, int32_t total_q, int32_t causal, int32_t window, int32_t sinks,
+                         float sm_scale, void* workspace, int num_sms, cudaStream_t stream);
 const DeviceInfo* device_info() {
   static DeviceInfo info[64];
   static bool known[64] = {};
@@ -467,7 +467,67 @@ int coopt_paged_chunked(const coopt_cache* cache, const void* q, void* out, cons
     return launch_decode(a, static_cast<cudaStream_t>(stream));
   }
   return launch_paged_prefill(cache, q, out, cu_q_lens, block_table, max_blocks_per_seq, context_lens, batch,
-                              num_q_heads, total_q, causal, sm_scale, workspace, num_sms(), static_cast<cudaStream_t>(stream));
+                              num_q_heads, total_q, causal, 0, 0, sm_scale, workspace, num_sms(), static_cast<cudaStream_t>(stream));
+}
+
+// Windows and sinks beyond any context mean the same as the longest one; sums of them and positions stay inside 32 bits.
+static int32_t within_context(int32_t tokens) { return std::min(tokens, 1 << 29); }
+static int check_window_args(int32_t window, int32_t sinks, int32_t max_blocks_per_seq) {
+  if (window <= 0 || sinks < 0) return COOPT_ERR_INVALID_ARG;
+  return max_blocks_per_seq > (1 << 29) / kBlockSize ? COOPT_ERR_UNSUPPORTED : COOPT_OK;
+}
+
+int coopt_window_decode(const coopt_cache* cache, const void* k_new, const void* v_new, int64_t kv_token_stride,
+                        const int64_t* slot_mapping, const void* q, void* out, const int32_t* block_table,
+                        int32_t max_blocks_per_seq, const int32_t* context_lens, int32_t batch, int32_t num_q_heads,
+                        int32_t window, int32_t sinks, float sm_scale, void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = check_attention_args(cache, q, out, block_table, max_blocks_per_seq, context_lens, batch, num_q_heads);
+  if (rc != COOPT_OK) return rc;
+  rc = check_window_args(window, sinks, max_blocks_per_seq);
+  if (rc != COOPT_OK) return rc;
+  const bool append = k_new || v_new || slot_mapping;
+  if (append && (!k_new || !v_new || !slot_mapping || kv_token_stride < static_cast<int64_t>(cache->num_kv_heads) * cache->head_dim))
+    return COOPT_ERR_INVALID_ARG;
+  if (batch == 0) return COOPT_OK;
+  if (!workspace || workspace_bytes < workspace_need(batch, num_q_heads, cache->num_kv_heads, cache->head_dim, max_blocks_per_seq, 0, 1))
+    return COOPT_ERR_WORKSPACE;
+  coopt_layer_io io = {cache, k_new, v_new, slot_mapping, q, out};
+  DecodeOrder order = kDependent;
+  if (append && !is_fp8(cache->dtype)) {
+    // bf16 tokens are stored as they are, by a launch of their own
+    rc = launch_kv_write(cache, k_new, v_new, kv_token_stride, slot_mapping, batch, static_cast<cudaStream_t>(stream));
+    if (rc != COOPT_OK) return rc;
+    io.k_new = io.v_new = nullptr;
+    io.slot_mapping = nullptr;
+    order = kAfterWrite;
+  }
+  DecodeCall a = attention_call(&io, 1, max_blocks_per_seq, batch, num_q_heads, 0, sm_scale, workspace);
+  a.block_table = block_table;
+  a.context_lens = context_lens;
+  a.kv_token_stride = kv_token_stride;
+  a.window = within_context(window);
+  a.sinks = within_context(sinks);
+  a.order = order;
+  // no sequence lists more blocks than its sinks and its window touch
+  const int32_t listed = std::min(max_blocks_per_seq, sink_blocks(a.sinks) + a.window / kBlockSize + 2);
+  a.shares = shares_of(batch, cache->num_kv_heads, listed, 0);
+  return launch_decode(a, static_cast<cudaStream_t>(stream));
+}
+
+int coopt_window_prefill(const coopt_cache* cache, const void* q, void* out, const int32_t* cu_q_lens, const int32_t* block_table,
+                         int32_t max_blocks_per_seq, const int32_t* context_lens, int32_t batch, int32_t num_q_heads,
+                         int32_t total_q, int32_t window, int32_t sinks, float sm_scale, void* workspace, size_t workspace_bytes,
+                         void* stream) {
+  int rc = check_attention_args(cache, q, out, block_table, max_blocks_per_seq, context_lens, batch, num_q_heads);
+  if (rc != COOPT_OK) return rc;
+  if (!cu_q_lens || total_q < 0) return COOPT_ERR_INVALID_ARG;
+  rc = check_window_args(window, sinks, max_blocks_per_seq);
+  if (rc != COOPT_OK) return rc;
+  if (!is_fp8(cache->dtype)) return COOPT_ERR_UNSUPPORTED;
+  if (batch == 0 || total_q == 0) return COOPT_OK;
+  if (!workspace || workspace_bytes < workspace_control_bytes()) return COOPT_ERR_WORKSPACE;
+  return launch_paged_prefill(cache, q, out, cu_q_lens, block_table, max_blocks_per_seq, context_lens, batch, num_q_heads, total_q, 1,
+                              within_context(window), within_context(sinks), sm_scale, workspace, num_sms(), static_cast<cudaStream_t>(stream));
 }
 
 namespace {
@@ -562,10 +622,11 @@ const char* coopt_status_string(int status) {
     case COOPT_ERR_WORKSPACE: return "workspace missing or too small";
     case COOPT_ERR_CUDA: return "CUDA runtime error";
     case COOPT_ERR_TIMEOUT: return "device-side wait timed out";
+    case COOPT_ERR_PAGES: return "too few free blocks in the pool";
     default: return "unknown status";
   }
 }
 
-int coopt_version(void) { return 200; }
+int coopt_version(void) { return 210; }
 
 }  // extern "C"

@@ -75,9 +75,11 @@ struct Cfg {
   static constexpr int kMiscOff = kRecOff + kWarps * 32;
   static constexpr int kCopyWalkOff = kMiscOff + 192;           // walks of a warp: where its copies are, and where its work is
   static constexpr int kSmemBytes = kCopyWalkOff + kWarps * 128;
+  static constexpr int kGapOff = kSmemBytes;                    // windowed calls: blocks that each sequence passes over
+  static constexpr int kWindowSmemBytes = kGapOff + kMaxBatch * 4;
   static_assert(kGran % 128 == 0 && kPiece % 128 == 0 && kStages * kGran >= kPiece && kWarpBytes % 128 == 0 && kCopy % 16 == 0, "copies land on 128-byte boundaries");
-  static_assert(kStages >= 2 && kSmemBytes <= kMaxSmem, "room for copies in flight");
-  static_assert(kCtasPerSm * (kSmemBytes + 1024) <= 233472, "shared memory of one SM");
+  static_assert(kStages >= 2 && kWindowSmemBytes <= kMaxSmem, "room for copies in flight");
+  static_assert(kCtasPerSm * (kWindowSmemBytes + 1024) <= 233472, "shared memory of one SM");
 };
 
 // What a warp leaves about the (at most two) units it holds only a piece of.
@@ -408,13 +410,14 @@ struct Merge {
   }
 };
 
-template <int D, int FMT, int L>
+template <int D, int FMT, int L, bool kWindow>
 __global__ void __launch_bounds__(Cfg<D, FMT>::kThreads, kCtasPerSm) paged_decode_kernel(const __grid_constant__ DecodeParams p, const __grid_constant__ LayerTable<L> table) {
   using C = Cfg<D, FMT>;
   constexpr int kQSteps = D / 16;
   extern __shared__ __align__(128) uint8_t smem[];
   int* lens = reinterpret_cast<int*>(smem + C::kLensOff);
   unsigned* pre = reinterpret_cast<unsigned*>(smem + C::kPreOff);
+  [[maybe_unused]] int* gaps = reinterpret_cast<int*>(smem + C::kGapOff);
   Rec* recs = reinterpret_cast<Rec*>(smem + C::kRecOff);
   int* misc = reinterpret_cast<int*>(smem + C::kMiscOff);   // [0..15] warps' sums, [16] wrong plan, [17..32] warps' longest unit
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -461,6 +464,11 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kThreads, kCtasPerSm) paged_decod
       const int b = tid * kPer + k;
       int len = b < B ? p.context_lens[b] : 0;
       len = max(0, min(len, p.max_blocks_per_seq * kBlockSize));
+      if constexpr (kWindow) {
+        const int gap = window_gap(len - p.window, p.sinks);
+        if (b < B) gaps[b] = gap;
+        len -= gap * kBlockSize;
+      }
       if (b < B) lens[b] = len;
       const int nb = (len + kBlockSize - 1) / kBlockSize;
       const int units = nb == 0 ? 0 : (chunk == kNoChunks ? 1 : (nb + chunk - 1) / chunk);
@@ -600,6 +608,10 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kThreads, kCtasPerSm) paged_decod
   const int fy = share_layer(ps);
   int ids_a = 0, g_a = 0, y_a = 0;
   int cnt_a = 0, pos_a = 0, ids_b = 0, cnt_b = 0, g_b = 0, y_b = 0;
+  auto table_at = [&](int b, int j) -> size_t {                         // block j of what is listed of a sequence
+    if constexpr (kWindow) j += j >= sink_blocks(p.sinks) ? gaps[b] : 0;
+    return static_cast<size_t>(b) * p.max_blocks_per_seq + j;
+  };
   auto prefetch_q = [&](int y, int b, int g) {
     if (lane < G * D / 64) prefetch_l2(reinterpret_cast<const uint8_t*>(layer(y).q + (static_cast<size_t>(b) * Hq + g * G) * D) + lane * 128);
   };
@@ -611,7 +623,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kThreads, kCtasPerSm) paged_decod
     cnt_b = min(32, pw.jend - pw.j);
     g_b = pw.g;
     y_b = share_layer(ps);
-    ids_b = lane < cnt_b ? p.block_table[static_cast<size_t>(pw.b) * p.max_blocks_per_seq + pw.u + pw.j + lane] : 0;
+    ids_b = lane < cnt_b ? p.block_table[table_at(pw.b, pw.u + pw.j + lane)] : 0;
     pw.j += cnt_b;
     if (pw.j >= pw.jend) {
       walk_on(ps, pw);
@@ -766,6 +778,13 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kThreads, kCtasPerSm) paged_decod
       // (The one test that every block meets: whether it is the last of the context.)
       const bool last = (j + 1) * kBlockSize >= valid;
       int seen = kBlockSize;                                                 // tokens of the block (Eq. 9)
+      // windowed: the tokens [hide, show) of the block lie between the sinks and the window
+      [[maybe_unused]] int hide = 0, show = 0;
+      if constexpr (kWindow) {
+        hide = max(0, p.sinks - j * kBlockSize);
+        show = min(kBlockSize, valid - p.window - j * kBlockSize);
+      }
+      const bool hidden = kWindow && hide < show;
       // the step's new token: what it needs is loaded while its block is on the way
       bool append = false;
       long long slot = -1;
@@ -780,7 +799,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kThreads, kCtasPerSm) paged_decod
             const bool vec = ((reinterpret_cast<uintptr_t>(io.k_new) | reinterpret_cast<uintptr_t>(io.v_new) | static_cast<uintptr_t>(p.kv_token_stride * 2)) & (D / 16 - 1)) == 0;
             const long long at = static_cast<long long>(work_walk->b) * p.kv_token_stride + work_walk->g * D;
             slot = io.slot_mapping[work_walk->b];
-            id = p.block_table[static_cast<size_t>(work_walk->b) * p.max_blocks_per_seq + work_walk->u + j];
+            id = p.block_table[table_at(work_walk->b, work_walk->u + j)];
             k_row = load_new<D>(io.k_new + at, vec, lane);
             v_row = load_new<D>(io.v_new + at, vec, lane);
           }
@@ -809,8 +828,11 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kThreads, kCtasPerSm) paged_decod
             }
             __syncwarp();
           }
-          if (seen < kBlockSize) {                 // V codes of slots past the context are cleared: they may hold anything
-            auto mask = [&](int word) { return seen >= 4 * word + 4 ? 0xFFFFFFFFu : seen <= 4 * word ? 0u : (1u << (8 * (seen - 4 * word))) - 1u; };
+        }
+        if (kWindow ? hidden || seen < kBlockSize : last) {
+          if (kWindow || seen < kBlockSize) {      // V codes of slots past the context are cleared: they may hold anything (so may hidden ones)
+            auto below = [&](int n, int word) { return n >= 4 * word + 4 ? 0xFFFFFFFFu : n <= 4 * word ? 0u : (1u << (8 * (n - 4 * word))) - 1u; };
+            auto mask = [&](int word) { return hidden ? below(seen, word) & (below(hide, word) | ~below(show, word)) : below(seen, word); };
 #pragma unroll
             for (int i = 0; i < D / 32; ++i) {
               uint4* row = reinterpret_cast<uint4*>(st + kBlockSize * D) + i * 32 + lane;        // 16 tokens of a dim
@@ -853,6 +875,10 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kThreads, kCtasPerSm) paged_decod
       if (seen < kBlockSize) {
         if (tok0 >= seen) x[0] = x[1] = -INFINITY;
         if (tok0 + kTokStep >= seen) x[2] = x[3] = -INFINITY;
+      }
+      if (hidden) {
+        if (tok0 >= hide && tok0 < show) x[0] = x[1] = -INFINITY;
+        if (tok0 + kTokStep >= hide && tok0 + kTokStep < show) x[2] = x[3] = -INFINITY;
       }
       const float t0 = fmaxf(x[0], x[2]), t1 = fmaxf(x[1], x[3]);
       if constexpr (L == 1) {                      // (for exported partials)
@@ -910,6 +936,11 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kThreads, kCtasPerSm) paged_decod
         if (seen < kBlockSize) {
           m0 = (2 * quad < seen ? 0x0000FFFFu : 0u) | (2 * quad + 1 < seen ? 0xFFFF0000u : 0u);
           m1 = (2 * quad + 8 < seen ? 0x0000FFFFu : 0u) | (2 * quad + 9 < seen ? 0xFFFF0000u : 0u);
+        }
+        if (hidden) {
+          auto shown = [&](int t) { return t < hide || t >= show; };
+          m0 &= (shown(2 * quad) ? 0x0000FFFFu : 0u) | (shown(2 * quad + 1) ? 0xFFFF0000u : 0u);
+          m1 &= (shown(2 * quad + 8) ? 0x0000FFFFu : 0u) | (shown(2 * quad + 9) ? 0xFFFF0000u : 0u);
         }
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
@@ -1099,11 +1130,12 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kThreads, kCtasPerSm) paged_decod
   }
 }
 
-template <int D, int FMT, int L>
+template <int D, int FMT, int L, bool kWindow>
 int launch_one(const DecodeParams& p, const LayerTable<L>& table, int grid, cudaStream_t stream) {
   using C = Cfg<D, FMT>;
-  if (!configure_kernel_smem(reinterpret_cast<const void*>(&paged_decode_kernel<D, FMT, L>), C::kSmemBytes)) return COOPT_ERR_CUDA;
-  return launch_dependent(paged_decode_kernel<D, FMT, L>, grid, C::kThreads, C::kSmemBytes, stream, p, table) ? COOPT_OK : COOPT_ERR_CUDA;
+  constexpr int kSmem = kWindow ? C::kWindowSmemBytes : C::kSmemBytes;
+  if (!configure_kernel_smem(reinterpret_cast<const void*>(&paged_decode_kernel<D, FMT, L, kWindow>), kSmem)) return COOPT_ERR_CUDA;
+  return launch_dependent(paged_decode_kernel<D, FMT, L, kWindow>, grid, C::kThreads, kSmem, stream, p, table) ? COOPT_OK : COOPT_ERR_CUDA;
 }
 
 // coopt_decode_plan: a copy of the step's context lengths and of the valid part of its block table, with the block ids
@@ -1161,12 +1193,12 @@ static int launch_layers(const DecodeParams& p, const coopt_layer_io* io, int gr
     if (p.layers > 1) {
       LayerTable<kManyLayers> table = {};
       fill(table.l);
-      return launch_one<D, FMT, kManyLayers>(p, table, grid, stream);
+      return launch_one<D, FMT, kManyLayers, false>(p, table, grid, stream);
     }
   }
   LayerTable<1> table;
   fill(table.l);
-  return launch_one<D, FMT, 1>(p, table, grid, stream);
+  return p.window > 0 ? launch_one<D, FMT, 1, true>(p, table, grid, stream) : launch_one<D, FMT, 1, false>(p, table, grid, stream);
 }
 static int launch_attention(const DecodeParams& p, const coopt_layer_io* io, int head_dim, int dtype, int grid, cudaStream_t stream) {
   if (head_dim == 128) {
@@ -1240,6 +1272,8 @@ int launch_decode(const DecodeCall& a, cudaStream_t stream) {
   p.num_blocks = c->num_blocks;
   p.solo_blocks = std::max(kSoloUnits, std::min(kSoloMost, a.batch * c->num_kv_heads / kSoloShare));
   p.sm_scale_log2 = a.sm_scale * kLog2e;
+  p.window = a.window;
+  p.sinks = a.sinks;
   p.chunk_blocks = a.chunk_size / kBlockSize;
   p.max_chunks = a.chunk_size > 0 ? static_cast<int>((static_cast<long long>(a.max_blocks_per_seq) * kBlockSize + a.chunk_size - 1) / a.chunk_size) : 0;
   if (a.plan != nullptr) {

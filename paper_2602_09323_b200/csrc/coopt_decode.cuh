@@ -69,6 +69,17 @@ __host__ __device__ inline int plan_key(int batch, int num_kv_heads, int chunk_b
   return static_cast<int>(h | 1u);
 }
 
+// Attention with a window and sinks.  Of a sequence only the blocks that hold one of the first `sinks` tokens and those from
+// the window's first token on are listed; what lies between is passed over.  So the line, and all that follows from it, knows a
+// sequence by the blocks that it keeps: block v of the shorter sequence is block v, or v + gap from the sinks' blocks on, of
+// the context.  Since whole blocks are left out, the token at position t >= window of the context has position t - 16 gap, and
+// "one of the first sinks tokens, or less than `window` behind the last" reads the same in either count.
+__host__ __device__ inline int sink_blocks(int sinks) { return (sinks + kBlockSize - 1) / kBlockSize; }
+__host__ __device__ inline int window_gap(int first, int sinks) {      // first: position of the window's first token
+  const int gap = (first > 0 ? first : 0) / kBlockSize - sink_blocks(sinks);
+  return gap > 0 ? gap : 0;
+}
+
 // What a layer brings of its own.
 struct LayerPtrs {
   uint8_t* cache;
@@ -102,6 +113,7 @@ struct DecodeParams {
   int solo_blocks;         // units of at most so many blocks are held whole by a warp
   int order;               // DecodeOrder
   float sm_scale_log2;     // sm_scale * log2(e)
+  int window, sinks;       // windowed call: the last `window` tokens and the first `sinks` are seen; else unused
   int chunk_blocks;        // 0 = decode mode
   int max_chunks;
   int* status;
@@ -132,6 +144,7 @@ struct DecodeCall {
   const int32_t* cu_q_lens;
   int64_t kv_token_stride;
   int32_t max_blocks_per_seq, batch, num_q_heads, chunk_size;
+  int32_t window, sinks;            // window 0: the whole context
   float sm_scale;
   void* workspace;
   int shares;                       // decode_shares()

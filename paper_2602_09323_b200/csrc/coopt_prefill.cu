@@ -41,6 +41,7 @@
 // cycles (head_dim 64: 10,000).
 // Every wait is bounded; a wait that runs out is reported in the status word and all roles leave through the common exit,
 // which frees the tensor memory.
+#include "coopt_decode.cuh"
 #include "coopt_umma.cuh"
 
 namespace coopt {
@@ -71,6 +72,7 @@ struct PrefillParams {
   int causal;
   int by_length;           // more CTAs than the device holds at a time: the long ones first
   float sm_scale_log2;
+  int window, sinks;       // windowed call: a query sees the `window` tokens up to itself, and the first `sinks`; else unused
   int* status;
 };
 
@@ -147,7 +149,10 @@ __device__ __forceinline__ void arrive_one(uint64_t* bar) {
 // kTurns: the two tiles of a CTA take turns at the exponentials.  A launch with one tile a CTA has a kernel without that code, which
 // nothing waits in there but which costs all the same (256 new tokens behind 2 x 8192, G = 8, 115.4 / 113.2 us; 24 sequences of
 // 335..671 tokens, one head, 23.8 / 23.4).
-template <int D, bool kE5m2, bool kTurns>
+// kWindow: a query sees only the last `window` tokens up to itself and the first `sinks` ones.  The CTA goes through the blocks that
+// any of its queries sees, and counts keys as if the others were not there (window_gap); what is left of the rule are masks at
+// the window's lower edge.
+template <int D, bool kE5m2, bool kTurns, bool kWindow>
 __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const PrefillParams p, const __grid_constant__ CUtensorMap map_part,
                                                                     const __grid_constant__ CUtensorMap map_hdr) {
   using C = Cfg<D>;
@@ -281,7 +286,11 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  const int b = misc[0], q0 = misc[1], row_base = misc[4], n_new = misc[5], L = misc[6], g = misc[7];
+  const int b = misc[0], q0 = misc[1], row_base = misc[4], n_new = misc[5], g = misc[7];
+  // (window: blocks passed over between the sinks and the first query's window; L and all positions are counted without them)
+  [[maybe_unused]] const int window_first = misc[6] - n_new + q0 + 1 - p.window;
+  const int gap = kWindow ? window_gap(window_first, p.sinks) : 0;
+  const int L = misc[6] - gap * kBlockSize;
   // keys that any row of tile x may see (Eq. 1: K_{<=t}), and tiles of keys
   auto tile_queries = [&](int x) { return x < p.tiles ? max(0, min(TQ, n_new - q0 - x * TQ)) : 0; };
   auto tile_keys = [&](int x) {
@@ -373,6 +382,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
     // index of the last visible key of the row.  Rows past the tile's last query (their operand is zero, and they are never
     // stored) see everything, so that their warp takes the same unmasked path as its live rows.
     const int lim = live ? (p.causal ? min(L - 1, L - n_new + q0 + x * TQ + qi) : L - 1) : (1 << 30);
+    [[maybe_unused]] const int from = kWindow && live ? lim - p.window + 1 : 0;      // window: keys [sinks, from) are hidden
     const int halves = (tile_keys(x) + kHalf - 1) / kHalf, other_halves = (tile_keys(1 - x) + kHalf - 1) / kHalf;
     float m_ref = -INFINITY, m_use = 0.0f, l_row = 0.0f, v_ref = 0.0f;      // m_use: m_ref, or 0 before the first visible key
     bool ok = true;
@@ -396,6 +406,13 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
       if (visible < kHalf - 1) {
 #pragma unroll
         for (int j = 0; j < kHalf; ++j) s[j >> 5][j & 31] = j <= visible ? s[j >> 5][j & 31] : 0xFF800000u;      // -inf
+      }
+      if constexpr (kWindow) {
+        const int hide = p.sinks - h * kHalf, show = from - h * kHalf;
+        if (hide < kHalf && show > 0 && hide < show) {
+#pragma unroll
+          for (int j = 0; j < kHalf; ++j) s[j >> 5][j & 31] = j < hide || j >= show ? s[j >> 5][j & 31] : 0xFF800000u;
+        }
       }
       float m_tile = -INFINITY;
 #pragma unroll
@@ -555,10 +572,19 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
       const uint8_t* src = smem + C::kVOff + vs * C::kCodes + (d >> 3) * 128 + (d & 7) * 16;
       uint8_t* dst = smem + C::kV16Off + w2 * C::kOperand + (d >> 3) * 2048 + (d & 7) * 16;
       const int nkeys = kv_end - t * kTileKeys;
+      // (window: of the keys that no query of this CTA sees, too)
+      [[maybe_unused]] const int hide = p.sinks - t * kTileKeys, show = window_first - gap * kBlockSize - t * kTileKeys;
 #pragma unroll 1
       for (int c = wt / D; c < nb; c += 128 / D) {
         const uint4 v = *reinterpret_cast<const uint4*>(src + c * C::kPart);
         uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        if constexpr (kWindow) {
+          if (hide < (c + 1) * kBlockSize && show > c * kBlockSize) {
+            auto below = [&](int n) { return n >= 4 ? 0xFFFFFFFFu : (n <= 0 ? 0u : (1u << (8 * n)) - 1u); };
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] &= below(hide - c * kBlockSize - 4 * j) | ~below(show - c * kBlockSize - 4 * j);
+          }
+        }
         const int keep = nkeys - c * kBlockSize;
         if (keep < kBlockSize) {                          // the context ends inside this block: codes past it are cleared
 #pragma unroll
@@ -675,7 +701,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
       const int* trow = p.block_table + static_cast<size_t>(b) * p.max_blocks_per_seq;
       auto load_batch = [&](int lb) -> int {
         const int j = lb * 32 + lane;
-        int id = j < n_blocks ? trow[j] : 0;
+        int id = j < n_blocks ? trow[kWindow && j >= sink_blocks(p.sinks) ? j + gap : j] : 0;
         if (id < 0 || id >= p.num_blocks) { atomicCAS(p.status, 0, COOPT_ERR_INVALID_ARG); id = 0; }
         return id;
       };
@@ -774,7 +800,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
   if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
-template <int D, bool kE5m2>
+template <int D, bool kE5m2, bool kWindow>
 int launch_one(const coopt_cache* c, const PrefillParams& p, dim3 grid, cudaStream_t stream) {
   using C = Cfg<D>;
   CUtensorMap map_part, map_hdr;
@@ -785,17 +811,17 @@ int launch_one(const coopt_cache* c, const PrefillParams& p, dim3 grid, cudaStre
     if (!configure_kernel_smem(reinterpret_cast<const void*>(kernel), C::kSmemBytes)) return COOPT_ERR_CUDA;
     return launch_dependent(kernel, grid, kThreads, C::kSmemBytes, stream, p, map_part, map_hdr) ? COOPT_OK : COOPT_ERR_CUDA;
   };
-  return p.tiles == 2 ? launch(&paged_prefill_kernel<D, kE5m2, true>) : launch(&paged_prefill_kernel<D, kE5m2, false>);
+  return p.tiles == 2 ? launch(&paged_prefill_kernel<D, kE5m2, true, kWindow>) : launch(&paged_prefill_kernel<D, kE5m2, false, kWindow>);
 }
 
 }  // namespace
 
 int launch_paged_prefill(const coopt_cache* c, const void* q, void* out, const int32_t* cu_q_lens,
                          const int32_t* block_table, int32_t max_blocks_per_seq, const int32_t* context_lens,
-                         int32_t batch, int32_t num_q_heads, int32_t total_q, int32_t causal, float sm_scale,
-                         void* workspace, int num_sms, cudaStream_t stream) {
+                         int32_t batch, int32_t num_q_heads, int32_t total_q, int32_t causal, int32_t window, int32_t sinks,
+                         float sm_scale, void* workspace, int num_sms, cudaStream_t stream) {
   if (!is_fp8(c->dtype)) return COOPT_ERR_UNSUPPORTED;
-  if (c->dtype == COOPT_KV_FP8_E5M2 && c->head_dim != 128) return COOPT_ERR_UNSUPPORTED;
+  if (c->dtype == COOPT_KV_FP8_E5M2 && c->head_dim != 128 && window == 0) return COOPT_ERR_UNSUPPORTED;
   PrefillParams p;
   p.q = static_cast<const __nv_bfloat16*>(q);
   p.out = static_cast<__nv_bfloat16*>(out);
@@ -811,6 +837,8 @@ int launch_paged_prefill(const coopt_cache* c, const void* q, void* out, const i
   p.tile_queries = kRows / p.group;
   p.causal = causal;
   p.sm_scale_log2 = sm_scale * kLog2e;
+  p.window = window;
+  p.sinks = sinks;
   p.status = static_cast<int*>(workspace);
   auto most = [&](int tiles) { return static_cast<long long>(total_q) / (tiles * p.tile_queries) + batch; };   // every sequence adds at most one that is partly filled
   // A CTA with one tile takes about 0.73 of the time of one with two (the tensor core and the exponential units are less busy,
@@ -822,8 +850,13 @@ int launch_paged_prefill(const coopt_cache* c, const void* q, void* out, const i
   if (pairs * c->num_kv_heads > 0x7fffffffll) return COOPT_ERR_UNSUPPORTED;
   const dim3 grid(static_cast<unsigned>(pairs * c->num_kv_heads));
   p.by_length = pairs * c->num_kv_heads > num_sms ? 1 : 0;
-  if (c->head_dim == 64) return launch_one<64, false>(c, p, grid, stream);
-  return c->dtype == COOPT_KV_FP8_E5M2 ? launch_one<128, true>(c, p, grid, stream) : launch_one<128, false>(c, p, grid, stream);
+  const bool e5m2 = c->dtype == COOPT_KV_FP8_E5M2;
+  if (window > 0) {
+    if (c->head_dim == 64) return e5m2 ? launch_one<64, true, true>(c, p, grid, stream) : launch_one<64, false, true>(c, p, grid, stream);
+    return e5m2 ? launch_one<128, true, true>(c, p, grid, stream) : launch_one<128, false, true>(c, p, grid, stream);
+  }
+  if (c->head_dim == 64) return launch_one<64, false, false>(c, p, grid, stream);
+  return e5m2 ? launch_one<128, true, false>(c, p, grid, stream) : launch_one<128, false, false>(c, p, grid, stream);
 }
 
 }  // namespace coopt
