@@ -156,7 +156,7 @@ def _check(status: int, what: str) -> None:
 # A call of a small problem is as long as its way through this file (10 us for a kernel of 2), so what every call does is
 # kept cheap: the current stream's handle without a Stream object around it, addresses as plain integers (the argument
 # types convert them), dtypes compared by identity.
-_BF16, _I32, _I64 = torch.bfloat16, torch.int32, torch.int64
+_BF16, _I32, _I64, _U8 = torch.bfloat16, torch.int32, torch.int64, torch.uint8
 _current_device = getattr(torch._C, "_cuda_getDevice", None)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
@@ -412,27 +412,41 @@ def decode_step_host(cache: Cache, step_inputs: torch.Tensor, out: torch.Tensor,
 
 
 # ---- attention with a sliding window and sinks -------------------------------------------------------------------
-# The calls of this part and the next say what they do not take by ValueError, also under ``python -O``.
+# The calls of this part and the next say what they do not take by ValueError, also under ``python -O``.  The checks are one
+# expression a call (1 us; a function for each of them took 5); what exactly is wrong is looked for only if something is.
 
 def _need(ok: bool, what: str) -> None:
     if not ok:
         raise ValueError(what)
 
 
+def _device() -> int:
+    return torch.cuda.current_device() if _current_device is None else _current_device()
+
+
 def _here(*tensors) -> None:
     """Tensors of the current device, on which the call is enqueued."""
-    device = torch.cuda.current_device() if _current_device is None else _current_device()
     for t in tensors:
-        _need(t.is_cuda and t.get_device() == device, "every tensor has to be on the current CUDA device")
+        _need(t.get_device() == _device(), "every tensor has to be on the current CUDA device")
 
 
-def _window_inputs(cache: Cache, q, block_table, context_lens, workspace, out):
+def _window_inputs(cache: Cache, q, block_table, context_lens, workspace, out, rows) -> None:
     _here(cache.data, q, block_table, context_lens, workspace, out)
     _need(q.dtype is _BF16 and q.is_contiguous() and q.dim() == 3 and q.shape[2] == cache.head_dim, "q: contiguous bf16 [rows, heads, head_dim]")
     _need(out.dtype is _BF16 and out.is_contiguous() and out.shape == q.shape, "out: like q")
     _need(block_table.dtype is _I32 and block_table.is_contiguous() and block_table.dim() == 2, "block_table: contiguous int32 [batch, width]")
     _need(context_lens.dtype is _I32 and context_lens.is_contiguous() and context_lens.numel() == block_table.shape[0],
           "context_lens: contiguous int32, one per row of the table")
+    _need(workspace.dtype is torch.uint8 and workspace.is_contiguous(), "workspace: contiguous uint8")
+    _need(rows is None or rows == block_table.shape[0], "one query row per row of the table")
+
+
+def _window_ok(cache: Cache, q, table, lens, ws, out) -> bool:
+    device = _device()
+    return (q.get_device() == device and out.get_device() == device and table.get_device() == device and lens.get_device() == device
+            and ws.get_device() == device and cache.data.get_device() == device and q.dtype is _BF16 and out.dtype is _BF16 and table.dtype is _I32
+            and lens.dtype is _I32 and ws.dtype is _U8 and q.is_contiguous() and out.is_contiguous() and table.is_contiguous() and lens.is_contiguous()
+            and ws.is_contiguous())
 
 
 def window_decode(cache: Cache, q: torch.Tensor, block_table: torch.Tensor, context_lens: torch.Tensor, window: int, sinks: int,
@@ -442,23 +456,27 @@ def window_decode(cache: Cache, q: torch.Tensor, block_table: torch.Tensor, cont
     (bf16 [B, Hkv, D], token stride taken from the tensor) and slot_mapping (int64 [B]) the new tokens are written first."""
     if out is None:
         out = torch.empty_like(q)
-    _window_inputs(cache, q, block_table, context_lens, workspace, out)
-    _need(q.shape[0] == block_table.shape[0], "one query row per row of the table")
-    stride, new = 0, (None, None, None)
+    shape, width = q.shape, block_table.shape
+    if not (_window_ok(cache, q, block_table, context_lens, workspace, out) and len(shape) == 3 and len(width) == 2 and shape[2] == cache.head_dim
+            and out.shape == shape and shape[0] == width[0] == context_lens.numel()):
+        _window_inputs(cache, q, block_table, context_lens, workspace, out, q.shape[0])
+    stride, k, v, slots = 0, None, None, None
     if k_new is not None or v_new is not None or slot_mapping is not None:
         _need(k_new is not None and v_new is not None and slot_mapping is not None, "k_new, v_new and slot_mapping go together")
+        rows, heads, at = shape[0], cache.num_kv_heads, k_new.stride()
+        if not (k_new.shape == v_new.shape == (rows, heads, shape[2]) and k_new.dtype is _BF16 and v_new.dtype is _BF16 and at == v_new.stride()
+                and at[2] == 1 and (at[1] == shape[2] or heads == 1)):
+            raise ValueError("k_new, v_new: bf16 [B, Hkv, D] of the same strides, heads and dims dense")
+        if not (slot_mapping.dtype is _I64 and slot_mapping.is_contiguous() and slot_mapping.numel() == rows):
+            raise ValueError("slot_mapping: contiguous int64 [B]")
         _here(k_new, v_new, slot_mapping)
-        shape = (q.shape[0], cache.num_kv_heads, cache.head_dim)
-        _need(k_new.dtype is _BF16 and v_new.dtype is _BF16 and k_new.shape == shape and v_new.shape == shape, "k_new, v_new: bf16 [B, Hkv, D]")
-        at = k_new.stride()
-        _need(at == v_new.stride() and at[2] == 1 and (at[1] == shape[2] or shape[1] == 1), "k_new, v_new: the same strides, heads and dims dense")
-        _need(slot_mapping.dtype is _I64 and slot_mapping.is_contiguous() and slot_mapping.numel() == shape[0], "slot_mapping: contiguous int64 [B]")
-        stride = at[0] if shape[0] > 1 else shape[1] * shape[2]
-        new = (k_new.data_ptr(), v_new.data_ptr(), slot_mapping.data_ptr())
-    st = load_library().coopt_window_decode(cache.ref(), new[0], new[1], stride, new[2], q.data_ptr(), out.data_ptr(), block_table.data_ptr(),
-                                            block_table.shape[1], context_lens.data_ptr(), q.shape[0], q.shape[1], int(window), int(sinks),
-                                            float(sm_scale), workspace.data_ptr(), workspace.numel(), _stream())
-    _check(st, "coopt_window_decode")
+        stride = at[0] if rows > 1 else heads * shape[2]
+        k, v, slots = k_new.data_ptr(), v_new.data_ptr(), slot_mapping.data_ptr()
+    st = load_library().coopt_window_decode(cache._ref, k, v, stride, slots, q.data_ptr(), out.data_ptr(), block_table.data_ptr(), width[1],
+                                            context_lens.data_ptr(), shape[0], shape[1], window, sinks, sm_scale, workspace.data_ptr(),
+                                            workspace.numel(), _stream())
+    if st != 0:
+        _check(st, "coopt_window_decode")
     return out
 
 
@@ -468,13 +486,18 @@ def window_prefill(cache: Cache, q: torch.Tensor, cu_q_lens: torch.Tensor, block
     ``sinks``; cu_q_lens int32 [B + 1] on the device.  Rows from cu_q_lens[B] on are left as they are."""
     if out is None:
         out = torch.empty_like(q)
-    _window_inputs(cache, q, block_table, context_lens, workspace, out)
+    shape, width = q.shape, block_table.shape
+    if not (_window_ok(cache, q, block_table, context_lens, workspace, out) and len(shape) == 3 and len(width) == 2 and shape[2] == cache.head_dim
+            and out.shape == shape and width[0] == context_lens.numel()):
+        _window_inputs(cache, q, block_table, context_lens, workspace, out, None)
+    if not (cu_q_lens.dtype is _I32 and cu_q_lens.is_contiguous() and cu_q_lens.numel() == width[0] + 1):
+        raise ValueError("cu_q_lens: contiguous int32 [B + 1]")
     _here(cu_q_lens)
-    _need(cu_q_lens.dtype is _I32 and cu_q_lens.is_contiguous() and cu_q_lens.numel() == block_table.shape[0] + 1, "cu_q_lens: contiguous int32 [B + 1]")
-    st = load_library().coopt_window_prefill(cache.ref(), q.data_ptr(), out.data_ptr(), cu_q_lens.data_ptr(), block_table.data_ptr(),
-                                             block_table.shape[1], context_lens.data_ptr(), block_table.shape[0], q.shape[1], q.shape[0],
-                                             int(window), int(sinks), float(sm_scale), workspace.data_ptr(), workspace.numel(), _stream())
-    _check(st, "coopt_window_prefill")
+    st = load_library().coopt_window_prefill(cache._ref, q.data_ptr(), out.data_ptr(), cu_q_lens.data_ptr(), block_table.data_ptr(), width[1],
+                                             context_lens.data_ptr(), width[0], shape[1], shape[0], window, sinks, sm_scale,
+                                             workspace.data_ptr(), workspace.numel(), _stream())
+    if st != 0:
+        _check(st, "coopt_window_prefill")
     return out
 
 
@@ -486,6 +509,8 @@ class CacheSet:
     def __init__(self, caches):
         self.keep = list(caches)
         self.array = (coopt_cache * len(self.keep))(*[c.desc for c in self.keep])
+        self.device = self.keep[0].data.get_device() if self.keep else None
+        _need(all(c.data.get_device() == self.device for c in self.keep), "all layers of a set are on one device")
 
 
 class Pages:
@@ -495,6 +520,8 @@ class Pages:
         for t, dims in ((refs, 1), (block_table, 2), (context_lens, 1)):
             _need(t.dtype is _I32 and t.is_contiguous() and t.dim() == dims, "refs, block_table, context_lens: contiguous int32 [blocks], [rows, width], [rows]")
         _need(context_lens.shape[0] == block_table.shape[0], "context_lens: one per row of the table")
+        self.device = refs.get_device()
+        _need(self.device == block_table.get_device() == context_lens.get_device(), "a pool is on one device")
         self.refs, self.block_table, self.context_lens = refs, block_table, context_lens
         rows, width = block_table.shape
         self.desc = coopt_pages(refs.data_ptr(), block_table.data_ptr(), context_lens.data_ptr(), refs.shape[0], rows, width)
@@ -520,62 +547,78 @@ def new_pages_workspace(num_blocks: int, rows: int, device: str = "cuda") -> tor
     return ws
 
 
-def _lists(*lists) -> None:
-    _here(*lists)
-    for t in lists:
-        _need(t.dtype is _I32 and t.is_contiguous() and t.dim() == 1 and t.shape == lists[0].shape, "lists of rows, lengths or blocks: contiguous int32 of one length")
+def _lists(device: int, a: torch.Tensor, b: torch.Tensor) -> int:
+    """The length of a call's two lists (of rows, lengths or blocks)."""
+    n = a.numel()
+    if not (a.dtype is _I32 and b.dtype is _I32 and a.dim() == b.dim() == 1 and b.numel() == n and a.is_contiguous() and b.is_contiguous()
+            and a.get_device() == b.get_device() == device):
+        raise ValueError("lists of rows, lengths or blocks: contiguous int32 of one length, on the current CUDA device")
+    return n
+
+
+def _pool_here(device: int, pages: Pages, workspace: torch.Tensor, caches: Optional[CacheSet] = None) -> None:
+    if not (pages.device == device == workspace.get_device() and workspace.dtype is _U8 and workspace.is_contiguous()
+            and (caches is None or caches.device is None or caches.device == device)):
+        raise ValueError("pool, caches and workspace (contiguous uint8) have to be on the current CUDA device")
 
 
 def pages_copy(caches: CacheSet, src: torch.Tensor, dst: torch.Tensor) -> None:
     """coopt_pages_copy: block src[i] copied over block dst[i] in every layer."""
-    _here(*(c.data for c in caches.keep))
-    _lists(src, dst)
-    st = load_library().coopt_pages_copy(caches.array, len(caches.keep), src.data_ptr(), dst.data_ptr(), src.shape[0], _stream())
-    _check(st, "coopt_pages_copy")
+    device = _device()
+    n = _lists(device, src, dst)
+    _need(caches.device == device, "caches: on the current CUDA device")
+    st = load_library().coopt_pages_copy(caches.array, len(caches.keep), src.data_ptr(), dst.data_ptr(), n, _stream())
+    if st != 0:
+        _check(st, "coopt_pages_copy")
 
 
 def pages_reserve(pages: Pages, row_ids: torch.Tensor, new_lens: torch.Tensor, workspace: torch.Tensor) -> None:
     """coopt_pages_reserve: row row_ids[i] gets blocks for new_lens[i] tokens, which becomes its length."""
-    _lists(row_ids, new_lens)
-    _here(pages.refs, workspace)
-    st = load_library().coopt_pages_reserve(pages.ref(), row_ids.data_ptr(), new_lens.data_ptr(), row_ids.shape[0], workspace.data_ptr(),
-                                            workspace.numel(), _stream())
-    _check(st, "coopt_pages_reserve")
+    device = _device()
+    n = _lists(device, row_ids, new_lens)
+    _pool_here(device, pages, workspace)
+    st = load_library().coopt_pages_reserve(pages._ref, row_ids.data_ptr(), new_lens.data_ptr(), n, workspace.data_ptr(), workspace.numel(), _stream())
+    if st != 0:
+        _check(st, "coopt_pages_reserve")
 
 
 def pages_fork(caches: CacheSet, pages: Pages, parents: torch.Tensor, children: torch.Tensor, workspace: torch.Tensor) -> None:
     """coopt_pages_fork: row children[i] becomes a copy of row parents[i] that shares its full blocks."""
-    _here(*(c.data for c in caches.keep))
-    _lists(parents, children)
-    _here(pages.refs, workspace)
-    st = load_library().coopt_pages_fork(caches.array, len(caches.keep), pages.ref(), parents.data_ptr(), children.data_ptr(), parents.shape[0],
+    device = _device()
+    n = _lists(device, parents, children)
+    _pool_here(device, pages, workspace, caches)
+    st = load_library().coopt_pages_fork(caches.array, len(caches.keep), pages._ref, parents.data_ptr(), children.data_ptr(), n,
                                          workspace.data_ptr(), workspace.numel(), _stream())
-    _check(st, "coopt_pages_fork")
+    if st != 0:
+        _check(st, "coopt_pages_fork")
 
 
 def pages_release(pages: Pages, row_ids: torch.Tensor, workspace: torch.Tensor, window: int = 0, sinks: int = 0) -> None:
     """coopt_pages_release: the rows' blocks are given back, all of them, or (window > 0) those outside window and sinks."""
-    _lists(row_ids)
-    _here(pages.refs, workspace)
-    st = load_library().coopt_pages_release(pages.ref(), row_ids.data_ptr(), row_ids.shape[0], int(window), int(sinks), workspace.data_ptr(),
-                                            workspace.numel(), _stream())
-    _check(st, "coopt_pages_release")
+    device = _device()
+    n = _lists(device, row_ids, row_ids)
+    _pool_here(device, pages, workspace)
+    st = load_library().coopt_pages_release(pages._ref, row_ids.data_ptr(), n, window, sinks, workspace.data_ptr(), workspace.numel(), _stream())
+    if st != 0:
+        _check(st, "coopt_pages_release")
 
 
 def pages_compact(caches: CacheSet, pages: Pages, workspace: torch.Tensor, table_out: Optional[torch.Tensor] = None,
                   refs_out: Optional[torch.Tensor] = None, used_out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """coopt_pages_compact: the blocks in use become the first ones of the pool; renumbered table and counts into table_out and
     refs_out (default: in place).  Returns the number of used blocks, an int32 tensor of one element."""
+    device = _device()
+    _pool_here(device, pages, workspace, caches)
     table_out = pages.block_table if table_out is None else table_out
     refs_out = pages.refs if refs_out is None else refs_out
     if used_out is None:
         used_out = torch.empty(1, dtype=_I32, device=pages.refs.device)
-    _here(*(c.data for c in caches.keep))
-    _here(pages.refs, workspace, table_out, refs_out, used_out)
-    for t, like in ((table_out, pages.block_table), (refs_out, pages.refs)):
-        _need(t.dtype is _I32 and t.is_contiguous() and t.shape == like.shape, "table_out, refs_out: like the pool's own")
-    _need(used_out.dtype is _I32 and used_out.numel() == 1, "used_out: one int32")
-    st = load_library().coopt_pages_compact(caches.array, len(caches.keep), pages.ref(), table_out.data_ptr(), refs_out.data_ptr(), used_out.data_ptr(),
+    if not (table_out.dtype is _I32 and refs_out.dtype is _I32 and used_out.dtype is _I32 and table_out.is_contiguous() and refs_out.is_contiguous()
+            and table_out.shape == pages.block_table.shape and refs_out.shape == pages.refs.shape and used_out.numel() == 1
+            and table_out.get_device() == refs_out.get_device() == used_out.get_device() == device):
+        raise ValueError("table_out, refs_out: like the pool's own; used_out: one int32; on the current CUDA device")
+    st = load_library().coopt_pages_compact(caches.array, len(caches.keep), pages._ref, table_out.data_ptr(), refs_out.data_ptr(), used_out.data_ptr(),
                                             workspace.data_ptr(), workspace.numel(), _stream())
-    _check(st, "coopt_pages_compact")
+    if st != 0:
+        _check(st, "coopt_pages_compact")
     return used_out

@@ -526,8 +526,10 @@ int coopt_window_prefill(const coopt_cache* cache, const void* q, void* out, con
   if (!is_fp8(cache->dtype)) return COOPT_ERR_UNSUPPORTED;
   if (batch == 0 || total_q == 0) return COOPT_OK;
   if (!workspace || workspace_bytes < workspace_control_bytes()) return COOPT_ERR_WORKSPACE;
+  window = within_context(window);
+  sinks = within_context(sinks);
   return launch_paged_prefill(cache, q, out, cu_q_lens, block_table, max_blocks_per_seq, context_lens, batch, num_q_heads, total_q, 1,
-                              within_context(window), within_context(sinks), sm_scale, workspace, num_sms(), static_cast<cudaStream_t>(stream));
+                              window, sinks, sm_scale, workspace, num_sms(), static_cast<cudaStream_t>(stream));
 }
 
 namespace {

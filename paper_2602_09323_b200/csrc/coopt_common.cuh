@@ -198,18 +198,25 @@ __device__ __forceinline__ void wait_previous_kernel() {
 }
 
 template <class Kernel, class... Args>
-bool launch_dependent(Kernel kernel, dim3 grid, int threads, int smem, cudaStream_t stream, const Args&... args) {
+bool launch_dependent_cluster(Kernel kernel, dim3 grid, int cluster, int threads, int smem, cudaStream_t stream, const Args&... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(static_cast<unsigned>(threads));
   cfg.dynamicSmemBytes = static_cast<size_t>(smem);
   cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = static_cast<unsigned>(cluster);
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess;
+}
+template <class Kernel, class... Args>
+bool launch_dependent(Kernel kernel, dim3 grid, int threads, int smem, cudaStream_t stream, const Args&... args) {
+  return launch_dependent_cluster(kernel, grid, 1, threads, smem, stream, args...);
 }
 
 #endif  // __CUDACC__

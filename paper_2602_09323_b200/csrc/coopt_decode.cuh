@@ -36,9 +36,9 @@ constexpr int kWholeUnits = 32;
 // 10.3 / 13.4 / 18.4 and 10.3 / 10.3 / 10.9 / 11.9), but a layer is cut the same way alone and in a launch over several, where
 // units that are not cut win throughout (eight layers of four sequences of 64 blocks 25.5 / 77.9; of one of 96 17.4 / 32.2).
 constexpr int kWholeUnitsIdle = 192;
-// .. and of a bf16 cache, which has no launch over several layers: blocks at either head dim.  (One sequence, 8 heads, head_dim
+// .. and of a bf16 cache, or in a windowed call, which have no launch over several layers: blocks at either head dim.  (One sequence, 8 heads, head_dim
 // 128, 32 / 48 / 64 blocks: 9.0 / 10.5 / 11.8 us not cut, 9.4 / 9.6 / 10.2 cut; head_dim 64: 8.6 / 9.7 / 10.8 and 9.0 / 9.3 / 10.0.)
-constexpr int kWholeUnitsIdleBf16 = 40;
+constexpr int kWholeUnitsIdleAlone = 40;
 // Units of at most so many blocks are not cut between warps either.  Eight layers of 40 sequences, 4 kv heads, us against units
 // spread over a CTA's warps: 1 block 10.6 / 27.6, 4 blocks 13.6 / 44, 8 blocks 17.5 / 65; one layer: 8.8 / 8.8, 11.7 / 10.5,
 // 14.0 / 10.5.

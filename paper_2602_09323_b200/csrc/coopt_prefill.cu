@@ -41,6 +41,9 @@
 // cycles (head_dim 64: 10,000).
 // Every wait is bounded; a wait that runs out is reported in the status word and all roles leave through the common exit,
 // which frees the tensor memory.
+#include <algorithm>
+#include <mutex>
+
 #include "coopt_decode.cuh"
 #include "coopt_umma.cuh"
 
@@ -54,6 +57,7 @@ constexpr int kWidenWarp = 8, kMmaWarp = 12, kCopyWarp = 14;      // warp 15: sc
 constexpr int kTileBlocks = 8;
 constexpr int kTileKeys = kTileBlocks * kBlockSize;        // 128: what is copied and widened at a time
 constexpr int kHalf = kTileKeys / 2;                       // 64: what is multiplied at a time
+constexpr int kMaxSplits = 8;                              // CTAs of a cluster
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kMaxLag = 11.0f;                           // a row's reference may lag its maximum by this much (base-2 logarithm units)
 constexpr float kScaleLag = 16.0f;                         // a V scale may exceed the reference scale by this factor
@@ -73,6 +77,7 @@ struct PrefillParams {
   int by_length;           // more CTAs than the device holds at a time: the long ones first
   float sm_scale_log2;
   int window, sinks;       // windowed call: a query sees the `window` tokens up to itself, and the first `sinks`; else unused
+  int splits;              // windowed call: CTAs (a cluster) that share the keys of one tile of queries
   int* status;
 };
 
@@ -146,6 +151,28 @@ __device__ __forceinline__ void arrive_one(uint64_t* bar) {
   asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n @q mbarrier.arrive.shared::cta.b64 _, [%0];\n}" ::"r"(smem_u32(bar)) : "memory");
 }
 
+// All threads of the cluster's CTAs; what they have written to shared memory before is seen by all behind it.
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// Shared memory of CTA `rank` of the cluster, at the place that has address `addr` here.
+__device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, int rank) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
+  return a;
+}
+__device__ __forceinline__ float2 ld_cluster_f2(uint32_t addr, int rank) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(cluster_addr(addr, rank)) : "memory");
+  return v;
+}
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr, int rank) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(cluster_addr(addr, rank)) : "memory");
+  return v;
+}
+
 // kTurns: the two tiles of a CTA take turns at the exponentials.  A launch with one tile a CTA has a kernel without that code, which
 // nothing waits in there but which costs all the same (256 new tokens behind 2 x 8192, G = 8, 115.4 / 113.2 us; 24 sequences of
 // 335..671 tokens, one head, 23.8 / 23.4).
@@ -156,6 +183,7 @@ template <int D, bool kE5m2, bool kTurns, bool kWindow>
 __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const PrefillParams p, const __grid_constant__ CUtensorMap map_part,
                                                                     const __grid_constant__ CUtensorMap map_hdr) {
   using C = Cfg<D>;
+  constexpr bool kSplit = kWindow && !kTurns;
   extern __shared__ __align__(128) uint8_t smem[];
   float* scales = reinterpret_cast<float*>(smem + C::kScaleOff);
   uint64_t* bar_kfull = reinterpret_cast<uint64_t*>(smem + C::kBarOff);   // K parts and headers of a tile have landed
@@ -216,7 +244,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
   // 187 and 94; 8 sequences of 4096 + 512 tokens take 427 and 431 us, 443 level by level.)
   if (warp == 0) {
     constexpr int kPer = 4, kBands = 8;
-    int left = blockIdx.x, found = -1, g = 0, q0 = 0, first = 0, count = 0, ctx = 0;
+    int left = kSplit ? blockIdx.x / p.splits : blockIdx.x, found = -1, g = 0, q0 = 0, first = 0, count = 0, ctx = 0;
     const int W = p.tiles * TQ;
     auto sequence = [&](int b, int& from, int& n, int& c) {
       from = b < p.batch ? p.cu_q_lens[b] : 0;
@@ -288,23 +316,34 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
   const uint32_t tmem = *tmem_slot;
   const int b = misc[0], q0 = misc[1], row_base = misc[4], n_new = misc[5], g = misc[7];
   // (window: blocks passed over between the sinks and the first query's window; L and all positions are counted without them)
-  [[maybe_unused]] const int window_first = misc[6] - n_new + q0 + 1 - p.window;
-  const int gap = kWindow ? window_gap(window_first, p.sinks) : 0;
-  const int L = misc[6] - gap * kBlockSize;
+  const int first_key = misc[6] - n_new + q0 + 1 - p.window;
+  const int gap = kWindow ? window_gap(first_key, p.sinks) : 0;
+  const int L_all = misc[6] - gap * kBlockSize;
   // keys that any row of tile x may see (Eq. 1: K_{<=t}), and tiles of keys
   auto tile_queries = [&](int x) { return x < p.tiles ? max(0, min(TQ, n_new - q0 - x * TQ)) : 0; };
-  auto tile_keys = [&](int x) {
+  auto all_keys = [&](int x) {
     const int nq = tile_queries(x);
-    return nq == 0 ? 0 : p.causal ? max(0, min(L, L - n_new + q0 + x * TQ + nq)) : L;
+    return nq == 0 ? 0 : p.causal ? max(0, min(L_all, L_all - n_new + q0 + x * TQ + nq)) : L_all;
   };
-  const int kv_end = max(tile_keys(0), tile_keys(1));
+  const int all_end = max(all_keys(0), all_keys(1)), all_tiles = (all_end + kTileKeys - 1) / kTileKeys;
+  // (split: this CTA's part of them, from which on keys are counted)
+  int key0 = 0, key1 = all_end;
+  if constexpr (kSplit) {
+    const int rank = blockIdx.x % p.splits;
+    key0 = all_tiles * rank / p.splits * kTileKeys;
+    key1 = min(all_end, all_tiles * (rank + 1) / p.splits * kTileKeys);
+  }
+  const int L = L_all - key0;
+  [[maybe_unused]] const int sinks = p.sinks - key0, window_first = first_key - gap * kBlockSize - key0;
+  auto tile_keys = [&](int x) { return kSplit ? max(0, min(all_keys(x), key1) - key0) : all_keys(x); };
+  const int kv_end = key1 - key0;
   const int n_blocks = (kv_end + kBlockSize - 1) / kBlockSize, n_tiles = (kv_end + kTileKeys - 1) / kTileKeys;
 
   const bool live = x < 2 && qi < tile_queries(x);
   const size_t grow = static_cast<size_t>(row_base + q0 + x * TQ + (live ? qi : 0)) * Hq + g * G + (live ? qh : 0);
   uint32_t pend_mask = 0, pend_par = 0;                 // copy lane: the latest phase expected of every slot it has filled
 
-  if (n_tiles == 0) {
+  if (all_tiles == 0) {
     // no such tile, or nothing visible: all-zero rows
     if (live)
       for (int d = 0; d < D; d += 8) *reinterpret_cast<uint4*>(p.out + grow * D + d) = make_uint4(0u, 0u, 0u, 0u);
@@ -408,7 +447,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
         for (int j = 0; j < kHalf; ++j) s[j >> 5][j & 31] = j <= visible ? s[j >> 5][j & 31] : 0xFF800000u;      // -inf
       }
       if constexpr (kWindow) {
-        const int hide = p.sinks - h * kHalf, show = from - h * kHalf;
+        const int hide = sinks - h * kHalf, show = from - h * kHalf;
         if (hide < kHalf && show > 0 && hide < show) {
 #pragma unroll
           for (int j = 0; j < kHalf; ++j) s[j >> 5][j & 31] = j < hide || j >= show ? s[j >> 5][j & 31] : 0xFF800000u;
@@ -502,6 +541,30 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
       const float k = l_row > 0.0f ? v_ref / l_row : 0.0f;
       // The rows go through shared memory, where the tile's query operand was (its products are done): 16 bytes of a row at
       // (chunk ^ row).
+      if constexpr (kSplit) {
+        if (p.splits > 1 && x == 0) {
+          // A part of the keys: the row normalised by its sum, with its maximum and sum, for the cluster to join.  (16 bytes of
+          // a row at chunk ^ row: a warp's stores meet every bank.)
+          constexpr int kChunks = D / 4;
+          float* part = reinterpret_cast<float*>(smem + C::kQOff) + r * D;
+#pragma unroll 1
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t o[32];
+            if (any_keys) {
+              tmem_ld32_issue(o_cols + 32 * c, o);
+              tmem_ld_wait32(o);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              auto f = [&](int e) { return k != 0.0f ? __uint_as_float(o[4 * j + e]) * k : 0.0f; };
+              *reinterpret_cast<float4*>(part + ((8 * c + j) ^ (r & (kChunks - 1))) * 4) = make_float4(f(0), f(1), f(2), f(3));
+            }
+          }
+          reinterpret_cast<float2*>(smem + C::kVOff)[r] = make_float2(m_ref, l_row);
+          tc_fence_before();
+        }
+      }
+      if (!kSplit || p.splits == 1) {
       constexpr int kLanes = D / 8, kRowsAt = 32 / kLanes;  // lanes of a row, rows at a time
       const int at = lane % kLanes, at_row = lane / kLanes;
       uint8_t* rows = smem + C::kQOff + x * C::kOperand + (warp & 3) * 32 * D * 2;
@@ -527,6 +590,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
           *reinterpret_cast<uint4*>(p.out + (tile_row + off) * D + at * 8) = *reinterpret_cast<const uint4*>(rows + row * D * 2 + (at ^ (row & (kLanes - 1))) * 16);
       }
       tc_fence_before();
+      }
     } else if (lane == 0) {
       atomicCAS(p.status, 0, COOPT_ERR_TIMEOUT);
     }
@@ -573,7 +637,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
       uint8_t* dst = smem + C::kV16Off + w2 * C::kOperand + (d >> 3) * 2048 + (d & 7) * 16;
       const int nkeys = kv_end - t * kTileKeys;
       // (window: of the keys that no query of this CTA sees, too)
-      [[maybe_unused]] const int hide = p.sinks - t * kTileKeys, show = window_first - gap * kBlockSize - t * kTileKeys;
+      [[maybe_unused]] const int hide = sinks - t * kTileKeys, show = window_first - t * kTileKeys;
 #pragma unroll 1
       for (int c = wt / D; c < nb; c += 128 / D) {
         const uint4 v = *reinterpret_cast<const uint4*>(src + c * C::kPart);
@@ -700,8 +764,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
       const CUtensorMap* map = what == 2 ? &map_hdr : &map_part;
       const int* trow = p.block_table + static_cast<size_t>(b) * p.max_blocks_per_seq;
       auto load_batch = [&](int lb) -> int {
-        const int j = lb * 32 + lane;
-        int id = j < n_blocks ? trow[kWindow && j >= sink_blocks(p.sinks) ? j + gap : j] : 0;
+        const int j = lb * 32 + lane, listed = j + key0 / kBlockSize;
+        int id = j < n_blocks ? trow[kWindow && listed >= sink_blocks(p.sinks) ? listed + gap : listed] : 0;
         if (id < 0 || id >= p.num_blocks) { atomicCAS(p.status, 0, COOPT_ERR_INVALID_ARG); id = 0; }
         return id;
       };
@@ -795,13 +859,90 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
     for (int i = 0; i < C::kVSlots; ++i)
       if ((pend_mask >> (4 + i)) & 1u) mbar_wait_bounded(&bar_vfull[i], (pend_par >> (4 + i)) & 1u);
   }
+  if constexpr (kSplit) {
+    if (p.splits > 1) {
+      // The cluster's CTAs join their parts by log-sum-exp, each an equal share of the rows, out of each other's shared memory
+      // (the softmax warps alone: the others have given their registers away).
+      cluster_sync();
+      if (warp < 8 && all_tiles > 0) {
+        constexpr int kChunks = D / 4, kAt = 32 / kChunks;     // lanes of a row, rows of a warp at a time
+        const int rank = blockIdx.x % p.splits, rows = tile_queries(0) * G, share = (rows + p.splits - 1) / p.splits;
+        const int chunk = lane % kChunks;
+        const uint32_t parts = smem_u32(smem + C::kQOff), sums = smem_u32(smem + C::kVOff);
+#pragma unroll 1
+        for (int i = warp * kAt + lane / kChunks; i < share; i += 8 * kAt) {
+          const int row = rank * share + i;
+          if (row >= rows) break;
+          float2 ml[kMaxSplits];
+          float4 o[kMaxSplits];
+          float top = -INFINITY;
+#pragma unroll
+          for (int s = 0; s < kMaxSplits; ++s) {
+            ml[s] = make_float2(-INFINITY, 0.0f);
+            if (s < p.splits) {
+              ml[s] = ld_cluster_f2(sums + row * 8, s);
+              o[s] = ld_cluster_f4(parts + (row * D + (chunk ^ (row & (kChunks - 1))) * 4) * 4, s);
+            }
+          }
+#pragma unroll
+          for (int s = 0; s < kMaxSplits; ++s)
+            if (ml[s].y > 0.0f) top = fmaxf(top, ml[s].x);
+          float den = 0.0f;
+          float4 num = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+          for (int s = 0; s < kMaxSplits; ++s) {
+            if (ml[s].y > 0.0f) {
+              const float w = ml[s].y * ex2(ml[s].x - top);
+              den += w;
+              num.x += w * o[s].x; num.y += w * o[s].y; num.z += w * o[s].z; num.w += w * o[s].w;
+            }
+          }
+          const float inv = den > 0.0f ? 1.0f / den : 0.0f;
+          const int q = row / G, h = row - q * G;
+          *reinterpret_cast<uint2*>(p.out + (static_cast<size_t>(row_base + q0 + q) * Hq + g * G + h) * D + 4 * chunk) =
+              make_uint2(pack_bf16x2(num.x * inv, num.y * inv), pack_bf16x2(num.z * inv, num.w * inv));
+        }
+      }
+      __syncwarp();
+      cluster_sync();                    // (nobody leaves while its rows are read)
+    }
+  }
   tc_fence_before();
   __syncthreads();
   if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
+// Clusters of that size that the device holds at a time; asked once.
+int clusters_at_once(const void* kernel, int size, int smem) {
+  static std::mutex mu;
+  static struct { const void* kernel; int dev, size, clusters; } known[512];
+  static int n = 0;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+  std::lock_guard<std::mutex> lock(mu);
+  for (int i = 0; i < n; ++i)
+    if (known[i].kernel == kernel && known[i].dev == dev && known[i].size == size) return known[i].clusters;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(size));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = static_cast<size_t>(smem);
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = static_cast<unsigned>(size);
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int clusters = 0;
+  if (cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) != cudaSuccess) {
+    (void)cudaGetLastError();
+    clusters = 0;
+  }
+  if (n < 512) known[n++] = {kernel, dev, size, clusters};
+  return clusters;
+}
+
 template <int D, bool kE5m2, bool kWindow>
-int launch_one(const coopt_cache* c, const PrefillParams& p, dim3 grid, cudaStream_t stream) {
+int launch_one(const coopt_cache* c, PrefillParams p, long long pairs, long long likely, long long key_tiles, cudaStream_t stream) {
   using C = Cfg<D>;
   CUtensorMap map_part, map_hdr;
   const long long granules = static_cast<long long>(c->num_blocks) * c->num_kv_heads;
@@ -809,7 +950,16 @@ int launch_one(const coopt_cache* c, const PrefillParams& p, dim3 grid, cudaStre
     return COOPT_ERR_CUDA;
   auto launch = [&](auto* kernel) {
     if (!configure_kernel_smem(reinterpret_cast<const void*>(kernel), C::kSmemBytes)) return COOPT_ERR_CUDA;
-    return launch_dependent(kernel, grid, kThreads, C::kSmemBytes, stream, p, map_part, map_hdr) ? COOPT_OK : COOPT_ERR_CUDA;
+    // Where the tiles leave room on the device, the keys of one are shared out to a cluster, as large as fits for all of them at
+    // once.  (n = 4 new tokens behind 9000, 40 heads over 8, head_dim 128, us with 1 / 2 / 3 / 5 / 8 CTAs: one sequence, window
+    // 4000 54.7 / 33.3 / 25.3 / 19.6 / 15.7, 1000 20.8 / 16.2 / 13.7 / 12.0 / 11.4, 250 11.9 / 11.4 / 10.6; eight sequences, 1000
+    // 21.9 / 17.2, and 27.9 with three, which do not fit at once.  Two tiles of keys are not worth it: 10.6 / 10.9.)
+    if (kWindow && p.tiles == 1 && key_tiles > 2)
+      for (int s = static_cast<int>(std::min<long long>(key_tiles, kMaxSplits)); s > 1 && p.splits == 1; --s)
+        if (likely <= clusters_at_once(reinterpret_cast<const void*>(kernel), s, C::kSmemBytes)) p.splits = s;
+    if (pairs * c->num_kv_heads * p.splits > 0x7fffffffll) return COOPT_ERR_UNSUPPORTED;
+    const dim3 grid(static_cast<unsigned>(pairs * c->num_kv_heads * p.splits));
+    return launch_dependent_cluster(kernel, grid, kWindow ? p.splits : 1, kThreads, C::kSmemBytes, stream, p, map_part, map_hdr) ? COOPT_OK : COOPT_ERR_CUDA;
   };
   return p.tiles == 2 ? launch(&paged_prefill_kernel<D, kE5m2, true, kWindow>) : launch(&paged_prefill_kernel<D, kE5m2, false, kWindow>);
 }
@@ -847,16 +997,23 @@ int launch_paged_prefill(const coopt_cache* c, const void* q, void* out, const i
   // would be 168 CTAs, 151 with two; 8 heads over 1, 128 behind 32000 508 / 370, 2048 alone 42.1 / 32.6.)
   p.tiles = most(1) * c->num_kv_heads <= num_sms ? 1 : 2;
   const long long pairs = most(p.tiles);
-  if (pairs * c->num_kv_heads > 0x7fffffffll) return COOPT_ERR_UNSUPPORTED;
-  const dim3 grid(static_cast<unsigned>(pairs * c->num_kv_heads));
   p.by_length = pairs * c->num_kv_heads > num_sms ? 1 : 0;
+  p.splits = 1;
+  // What decides on sharing the keys of a tile out (launch_one): query tiles there will probably be, where runs are short one a
+  // sequence, and tiles of keys that one of them goes through at most.
+  long long likely = 0, key_tiles = 0;
+  if (window > 0 && p.tiles == 1) {
+    likely = (2ll * total_q <= static_cast<long long>(batch) * p.tile_queries ? batch : most(1)) * c->num_kv_heads;
+    const long long keys = static_cast<long long>(window) + sinks + p.tile_queries + 2 * kBlockSize;
+    key_tiles = (std::min(keys, static_cast<long long>(max_blocks_per_seq) * kBlockSize) + kTileKeys - 1) / kTileKeys;
+  }
   const bool e5m2 = c->dtype == COOPT_KV_FP8_E5M2;
   if (window > 0) {
-    if (c->head_dim == 64) return e5m2 ? launch_one<64, true, true>(c, p, grid, stream) : launch_one<64, false, true>(c, p, grid, stream);
-    return e5m2 ? launch_one<128, true, true>(c, p, grid, stream) : launch_one<128, false, true>(c, p, grid, stream);
+    if (c->head_dim == 64) return e5m2 ? launch_one<64, true, true>(c, p, pairs, likely, key_tiles, stream) : launch_one<64, false, true>(c, p, pairs, likely, key_tiles, stream);
+    return e5m2 ? launch_one<128, true, true>(c, p, pairs, likely, key_tiles, stream) : launch_one<128, false, true>(c, p, pairs, likely, key_tiles, stream);
   }
-  if (c->head_dim == 64) return launch_one<64, false, false>(c, p, grid, stream);
-  return e5m2 ? launch_one<128, true, false>(c, p, grid, stream) : launch_one<128, false, false>(c, p, grid, stream);
+  if (c->head_dim == 64) return launch_one<64, false, false>(c, p, pairs, likely, key_tiles, stream);
+  return e5m2 ? launch_one<128, true, false>(c, p, pairs, likely, key_tiles, stream) : launch_one<128, false, false>(c, p, pairs, likely, key_tiles, stream);
 }
 
 }  // namespace coopt

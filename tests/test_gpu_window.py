@@ -143,11 +143,14 @@ def test_a_window_over_everything_is_the_call_without_one(fmt):
     want, _ = helpers.gpu_decode(w, cache)
     assert torch.equal(decode(w, cache, w.block_table, lens, 2000, 0), want)
     if fmt != "bf16":
-        w = workloads.make_workload("whole", [700, 33, 300], 10, 2, 128, seed=18, q_lens=[500, 2, 40])
-        cache = helpers.gpu_fill(w, FMT[fmt])
+        # (runs of query tokens: keys may be shared out to several CTAs, so both calls are held to the definition)
+        lens, q_lens = [700, 33, 300], [500, 2, 40]
+        w, cache, kv, table = make(lens, q_lens, 10, 2, 128, fmt, 700, 0, seed=18, poison=False)
+        ref, spread = attention.window_attention(w.q.float().numpy(), kv, w.block_table.numpy(), lens, 700, 0, w.cu_q_lens.numpy())
         ws = binding.new_workspace(3, 10, 2, 128, w.block_table.shape[1], 512, 542)
-        want = binding.paged_chunked(cache, w.q.cuda(), w.cu_q_lens.cuda(), w.block_table.cuda(), w.context_lens_tensor.cuda(), 512, True, w.sm_scale, ws)
-        assert torch.equal(prefill(w, cache, w.block_table, 700, 0), want)
+        whole = binding.paged_chunked(cache, w.q.cuda(), w.cu_q_lens.cuda(), w.block_table.cuda(), w.context_lens_tensor.cuda(), 512, True, w.sm_scale, ws)
+        for out in (whole, prefill(w, cache, w.block_table, 700, 0)):
+            check(out, ref, spread, fmt, prefill=True, vmax=6.0)
 
 
 @pytest.mark.parametrize("fmt,dim", [("e4m3", 128), ("e5m2", 64), ("bf16", 64)])
