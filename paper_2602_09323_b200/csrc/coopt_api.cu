@@ -45,6 +45,34 @@ bool configure_kernel_smem(const void* kernel, int bytes) {
   return true;
 }
 
+int clusters_at_once(const void* kernel, int size, int threads, int smem) {
+  struct Known { const void* kernel; int dev, size, clusters; };
+  static std::mutex mu;
+  static std::vector<Known> known;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+  std::lock_guard<std::mutex> lock(mu);
+  for (const Known& k : known)
+    if (k.kernel == kernel && k.dev == dev && k.size == size) return k.clusters;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(size));
+  cfg.blockDim = dim3(static_cast<unsigned>(threads));
+  cfg.dynamicSmemBytes = static_cast<size_t>(smem);
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = static_cast<unsigned>(size);
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int clusters = 0;
+  if (cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) != cudaSuccess) {
+    (void)cudaGetLastError();
+    clusters = 0;
+  }
+  known.push_back({kernel, dev, size, clusters});
+  return clusters;
+}
+
 namespace {
 
 bool cache_shape_ok(int head_dim, int block_size, int dtype) {

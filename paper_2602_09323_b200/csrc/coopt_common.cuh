@@ -190,6 +190,30 @@ __device__ __forceinline__ uint4 lds128(const void* p) {
   return v;
 }
 
+// ---- clusters -----------------------------------------------------------------------------------------
+constexpr int kMaxSplits = 8;      // CTAs of a cluster that share one piece of work
+// All threads of the cluster's CTAs; what they have written to shared memory before is seen by all behind it.
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// Shared memory of CTA `rank` of the cluster, at the place that has address `addr` here.
+__device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, int rank) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
+  return a;
+}
+__device__ __forceinline__ float2 ld_cluster_f2(uint32_t addr, int rank) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(cluster_addr(addr, rank)) : "memory");
+  return v;
+}
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr, int rank) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(cluster_addr(addr, rank)) : "memory");
+  return v;
+}
+
 // Launched as a programmatic dependent, a kernel may be set up while the one before it in the stream still runs: here it
 // waits until that one has finished, and lets the one behind it be set up.
 __device__ __forceinline__ void wait_previous_kernel() {
@@ -229,6 +253,8 @@ struct DeviceInfo {
 const DeviceInfo* device_info();  // cached per device; nullptr if the CUDA runtime fails
 // Raises a kernel's dynamic shared-memory limit once per (kernel, device); safe from several host threads.
 bool configure_kernel_smem(const void* kernel, int bytes);
+// Clusters of `size` CTAs that the current device holds at a time; asked once per (kernel, size, device).
+int clusters_at_once(const void* kernel, int size, int threads, int smem);
 // Host-side checks of a decode-style call: a coopt_status, nothing is enqueued.
 int check_attention_args(const coopt_cache* c, const void* q, void* out, const int32_t* block_table,
                          int32_t max_blocks_per_seq, const int32_t* context_lens, int32_t batch, int32_t num_q_heads);

@@ -48,7 +48,7 @@ constexpr float kShift = 8.0f, kUnshift = 1.0f / 256.0f;          // probabiliti
 
 constexpr int kMaxSmem = 232448;                                 // of a CTA
 
-template <int D, int FMT>
+template <int D, int FMT, int kPerSm = kCtasPerSm>
 struct Cfg {
   static constexpr bool kFp8 = FMT != COOPT_KV_BF16;
   [[maybe_unused]] static constexpr bool kE5m2 = FMT == COOPT_KV_FP8_E5M2;
@@ -57,7 +57,7 @@ struct Cfg {
   // sequences of 128..8192 tokens, four layers), 125.8 / 133.0 (four of 32768..131072 in chunks), 219.5 / 228.3 (32 x 4096, four
   // launches), 226.6 / 227.6 (eight layers of 32 x 2048), 32.1 / 32.4 (30 x 1597); head_dim 64, 4 / 5: 138.6 / 139.8 (64 of
   // 100..5000, G = 4, four layers), 17.1 / 17.3 (120 of 5..900).  bf16: 8 x 2 and 8 x 4 (182 registers).
-  static constexpr int kWarps = kFp8 ? (D == 128 ? 12 : 16) : 8;
+  static constexpr int kWarps = (kFp8 ? (D == 128 ? 12 : 16) : 8) / kPerSm;
   static constexpr int kThreads = kWarps * 32;
   static constexpr int kGran = granule_bytes(D, kFp8);
   static constexpr int kCopy = kFp8 ? 2 * kBlockSize * D + kFp8Header : kGran;   // bytes of a granule that are read
@@ -79,7 +79,7 @@ struct Cfg {
   static constexpr int kWindowSmemBytes = kGapOff + kMaxBatch * 4;
   static_assert(kGran % 128 == 0 && kPiece % 128 == 0 && kStages * kGran >= kPiece && kWarpBytes % 128 == 0 && kCopy % 16 == 0, "copies land on 128-byte boundaries");
   static_assert(kStages >= 2 && kWindowSmemBytes <= kMaxSmem, "room for copies in flight");
-  static_assert(kCtasPerSm * (kWindowSmemBytes + 1024) <= 233472, "shared memory of one SM");
+  static_assert(kPerSm * (kWindowSmemBytes + 1024) <= 233472, "shared memory of one SM");
 };
 
 // What a warp leaves about the (at most two) units it holds only a piece of.
@@ -410,9 +410,17 @@ struct Merge {
   }
 };
 
-template <int D, int FMT, int L, bool kWindow>
-__global__ void __launch_bounds__(Cfg<D, FMT>::kThreads, kCtasPerSm) paged_decode_kernel(const __grid_constant__ DecodeParams p, const __grid_constant__ LayerTable<L> table) {
-  using C = Cfg<D, FMT>;
+// kFewPerSm: a windowed call of few units.  No line is made of them: a unit has a CTA, of which so many fit an SM, or a cluster of
+// p.splits CTAs, every warp an equal part of its blocks, and the warps' and CTAs' pieces are joined through (distributed) shared
+// memory, so nothing goes through the workspace.  That is what short calls wait for most, and with two or three CTAs on an SM
+// one streams while another starts or joins.  (40 heads over 8, head_dim 128, E4M3, us as a line / so: one sequence, window 30
+// 11.3 / 5.6, 1024 12.3 / 7.2, 4096 14.2 / 9.7; 18 sequences, window 250 10.0 / 7.6, 2048 22.9 / 18.0; 32 sequences, two CTAs an
+// SM, window 250 16.0 / 9.2, 2048 32.9 / 27.7; 50, three, window 250 18.0 / 10.4.)
+template <int D, int FMT, int L, bool kWindow, int kFewPerSm>
+__global__ void __launch_bounds__(Cfg<D, FMT, kFewPerSm ? kFewPerSm : kCtasPerSm>::kThreads, kFewPerSm ? kFewPerSm : kCtasPerSm)
+paged_decode_kernel(const __grid_constant__ DecodeParams p, const __grid_constant__ LayerTable<L> table) {
+  constexpr bool kFew = kFewPerSm > 0;
+  using C = Cfg<D, FMT, kFewPerSm ? kFewPerSm : kCtasPerSm>;
   constexpr int kQSteps = D / 16;
   extern __shared__ __align__(128) uint8_t smem[];
   int* lens = reinterpret_cast<int*>(smem + C::kLensOff);
@@ -452,7 +460,20 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kThreads, kCtasPerSm) paged_decod
   if (p.order == kDependent) wait_previous_kernel();
 
   // ---- the line: context lengths and their prefix sums -------------------------------------------------------
-  {
+  int few_b = 0, few_g = 0, few_rank = 0;
+  if constexpr (kFew) {
+    const int unit = blockIdx.x / p.splits;
+    few_rank = blockIdx.x - unit * p.splits;
+    few_b = unit / Hkv;
+    few_g = unit - few_b * Hkv;
+    if (tid == 0) {
+      int len = max(0, min(p.context_lens[few_b], p.max_blocks_per_seq * kBlockSize));
+      gaps[few_b] = window_gap(len - p.window, p.sinks);
+      lens[few_b] = len - gaps[few_b] * kBlockSize;
+    }
+    if (lane < G) (reinterpret_cast<float*>(ring + piece0_off) + lane * C::kPieceStride)[D + 1] = 0.0f;       // (a warp without blocks has nothing)
+    __syncthreads();
+  } else {
     constexpr int kPer = (kMaxBatch + C::kThreads - 1) / C::kThreads;
     const int chunk = p.chunk_blocks > 0 ? p.chunk_blocks : kNoChunks;
     unsigned v[kPer], sum = 0;
@@ -497,7 +518,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kThreads, kCtasPerSm) paged_decod
     }
     __syncthreads();
   }
-  if (misc[16]) {                                  // not a plan of this problem (uniform over the grid)
+  if (!kFew && misc[16]) {                         // not a plan of this problem (uniform over the grid)
     if (p.order != kDependent) wait_previous_kernel();
     if (tid == 0) atomicCAS(p.status, 0, COOPT_ERR_INVALID_ARG);
     return;
@@ -508,14 +529,14 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kThreads, kCtasPerSm) paged_decod
   // A share: T places of a layer's line.  A layer is cut the same way whatever else the launch does, so its result does
   // not depend on how many layers share the launch.  CTA i takes the shares i, i + grid, .. of all layers, one layer
   // behind the other; the copies of a share are under way while the pieces of the one before are merged.
-  const unsigned places = Hkv * pre[B];
+  const unsigned places = kFew ? 0 : Hkv * pre[B];
   unsigned T = max(static_cast<unsigned>(kMinPlaces), (places + p.shares - 1) / p.shares);
   // Shared units cost a trip through the workspace at the end of a share.  Where units are short, a share holds the units
   // that begin among its places whole instead.  (In chunk mode every share between the first and the last of a (sequence,
   // kv head) has to hold a chunk of it.)
   int most = 0;
   bool none_empty = true;
-  for (int k = 0; k < C::kWarps; ++k) {
+  for (int k = 0; k < (kFew ? 0 : C::kWarps); ++k) {
     const int m = misc[17 + k];
     none_empty = none_empty && m < kSomeEmpty;
     most = max(most, m & (kSomeEmpty - 1));
@@ -532,7 +553,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kThreads, kCtasPerSm) paged_decod
   // (Three layers of 17 sequences of 854 tokens, two kv heads: 35.4 us with shares of 16 places, most of them empty and the
   // others unevenly spread over the CTAs, 14.1 so; eight of 7 sequences of 272..544 tokens, four kv heads: 29.7 / 20.5.)
   const bool by_unit = whole && !solo && p.chunk_blocks == 0 && T == kMinPlaces && none_empty && B * Hkv <= p.shares;
-  const unsigned shares = by_unit ? B * Hkv : (places + T - 1) / T, all_shares = L == 1 ? shares : shares * p.layers;
+  const unsigned shares = kFew ? gridDim.x : by_unit ? B * Hkv : (places + T - 1) / T, all_shares = L == 1 ? shares : shares * p.layers;
   // What is looked at seldom waits in shared memory, a copy for every warp, and not in registers that the loop over blocks
   // needs: the walk of the copies (once in 32 blocks), its share, and how shares are cut.
   Walk* copy_walk = reinterpret_cast<Walk*>(smem + C::kCopyWalkOff + warp * 128);
@@ -551,6 +572,14 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kThreads, kCtasPerSm) paged_decod
   };
   auto share_layer = [&](unsigned s) -> int { return L == 1 ? 0 : s / shares; };
   auto share_walk = [&](unsigned s, Walk& w) {                          // this warp's part of share s
+    if constexpr (kFew) {
+      const int nb = line_blocks(ln, few_b), all = p.splits * C::kWarps, at = few_rank * C::kWarps + warp;
+      w.b = few_b; w.g = few_g; w.nb = w.n = nb; w.u = 0; w.base = w.end = 0;
+      w.j = nb * at / all;
+      w.jend = nb * (at + 1) / all;
+      w.more = w.jend > w.j;
+      return;
+    }
     // (Three look-ups at most, in a loop: code that a CTA runs once is bound by the fetch of its instructions.)
     const unsigned T = cut[1], mode = cut[0];
     const bool solo = (mode & 2u) != 0;
@@ -593,6 +622,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kThreads, kCtasPerSm) paged_decod
     }
   };
   auto walk_on = [&](unsigned& s, Walk& w) {
+    if constexpr (kFew) { w.more = false; return; }
     walk_next(ln, w);
     walk_later(s, w);
   };
@@ -720,7 +750,12 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kThreads, kCtasPerSm) paged_decod
         if (p.cu_q_lens[b] != b) atomicCAS(p.status, 0, COOPT_ERR_INVALID_ARG);
   }
   // sequences with an empty context: all-zero output rows
-  for (int b = blockIdx.x; b < B; b += gridDim.x)
+  if constexpr (kFew) {
+    if (lens[few_b] == 0 && few_rank == 0)
+      for (int i = tid; i < G * D / 8; i += C::kThreads)
+        reinterpret_cast<uint4*>(layer(0).out + (static_cast<size_t>(few_b) * Hq + few_g * G) * D)[i] = make_uint4(0u, 0u, 0u, 0u);
+  }
+  for (int b = blockIdx.x; b < (kFew ? 0 : B); b += gridDim.x)
     if (lens[b] == 0)
       for (int y = 0; y < (L == 1 ? 1 : p.layers); ++y)
         for (int i = tid; i < Hq * D / 8; i += C::kThreads) reinterpret_cast<uint4*>(layer(y).out + static_cast<size_t>(b) * Hq * D)[i] = make_uint4(0u, 0u, 0u, 0u);
@@ -981,7 +1016,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kThreads, kCtasPerSm) paged_decod
       }
     }
     const bool starts = w.j == 0, ends = w.jend == w.n;
-    if (starts && ends && w.n == w.nb) {
+    if (!kFew && starts && ends && w.n == w.nb) {
       // the whole (sequence, kv head): bf16 rows, transposed so that a lane holds pairs of dims of head `row`
       __nv_bfloat16* dst = layer(y).out + (static_cast<size_t>(w.b) * Hq + w.g * G + row) * D + 2 * quad;
 #pragma unroll
@@ -993,7 +1028,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kThreads, kCtasPerSm) paged_decod
         }
       }
     }
-    if (starts && ends && p.chunk_blocks > 0) {
+    if (!kFew && starts && ends && p.chunk_blocks > 0) {
       // a whole chunk: exported
       const size_t rows = static_cast<size_t>(p.max_chunks);
       const size_t at = (static_cast<size_t>(w.b) * Hq + w.g * G + 2 * quad) * rows + w.u / ln.chunk;
@@ -1007,10 +1042,10 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kThreads, kCtasPerSm) paged_decod
         }
       }
     }
-    if (!(starts && ends)) {
+    if (kFew || !(starts && ends)) {
       // a piece: into shared memory, once the pieces of the share before are of no more use
       if (L > 1 && round > 0 && flags == 0 && !dead) dead = !__all_sync(0xffffffffu, mbar_wait_bounded(bar_merged, (round - 1) & 1u));
-      float* piece = reinterpret_cast<float*>(ring + (starts ? piece1_off : piece0_off));
+      float* piece = reinterpret_cast<float*>(ring + (starts && !kFew ? piece1_off : piece0_off));
       float* at = piece + 2 * quad * C::kPieceStride + row;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -1030,10 +1065,66 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kThreads, kCtasPerSm) paged_decod
       }
       flags |= starts ? kHas1 : kHas0 | (ends ? kEnds0 : 0);
     }
+    if constexpr (kFew) break;
     walk_next(ln, w);
   }
   COOPT_TRACE_CYCLES(p.trace, kTrWarpEnd + warp, lane == 0);
   COOPT_TRACE_VALUE(p.trace, kTrBlocks, tid == 0, consumed);
+  if constexpr (kFew) {
+    __syncthreads();
+    // A head to a warp: the pieces of this CTA's warps, then, over distributed shared memory, of the cluster's CTAs.
+    Merge<D, FMT, L> merge{p, table, ln, smem, recs, 0u, piece0_off, piece1_off, warp, lane, 0};
+    auto piece = [&](int k, int h) { return reinterpret_cast<float*>(smem + k * C::kWarpBytes + piece0_off) + h * C::kPieceStride; };
+    const int heads = lens[few_b] > 0 ? G : 0;
+#pragma unroll 1
+    for (int h = warp; h < heads; h += C::kWarps) {
+      Acc a;
+      acc_clear(a);
+      acc_merge<false>(a, C::kWarps, lane < C::kWarps ? piece(lane, h)[D] : 0.0f, lane < C::kWarps ? piece(lane, h)[D + 1] : 0.0f, merge.on(),
+                       [&](int k) { return piece(k, h) + lane * 4; });
+      if (p.splits == 1) {
+        merge.store_out(a, few_b, few_g, h);
+      } else {
+        __syncwarp();
+        if (merge.on()) *reinterpret_cast<float4*>(piece(0, h) + lane * 4) = a.num;
+        if (lane == 0) *reinterpret_cast<float2*>(piece(0, h) + D) = make_float2(a.M, a.den);
+      }
+    }
+    if (p.splits > 1) {
+      __syncwarp();
+      cluster_sync();
+#pragma unroll 1
+      for (int h = warp; h < heads; h += C::kWarps) {
+        if (h % p.splits != few_rank) continue;
+        const uint32_t at = smem_u32(piece(0, h));
+        float2 ml[kMaxSplits];
+        float4 o[kMaxSplits];
+        Acc a;
+        acc_clear(a);
+#pragma unroll
+        for (int s = 0; s < kMaxSplits; ++s) {
+          ml[s] = make_float2(-INFINITY, 0.0f);
+          if (s < p.splits) {
+            ml[s] = ld_cluster_f2(at + D * 4, s);
+            o[s] = ld_cluster_f4(at + (merge.on() ? lane : 0) * 16, s);
+          }
+          if (ml[s].y > 0.0f) a.M = fmaxf(a.M, ml[s].x);
+        }
+#pragma unroll
+        for (int s = 0; s < kMaxSplits; ++s) {
+          if (ml[s].y > 0.0f) {
+            const float f = ex2(ml[s].x - a.M);
+            a.den += ml[s].y * f;
+            a.num.x += o[s].x * f; a.num.y += o[s].y * f; a.num.z += o[s].z * f; a.num.w += o[s].w * f;
+          }
+        }
+        merge.store_out(a, few_b, few_g, h);
+      }
+      __syncwarp();
+      cluster_sync();                    // (nobody leaves while its pieces are read)
+    }
+    break;
+  }
   if ((cut[0] & 2u) != 0) break;         // solo: one share a CTA
   if (L == 1) {
     if (lane == 0) recs[warp].flags = flags;
@@ -1134,8 +1225,37 @@ template <int D, int FMT, int L, bool kWindow>
 int launch_one(const DecodeParams& p, const LayerTable<L>& table, int grid, cudaStream_t stream) {
   using C = Cfg<D, FMT>;
   constexpr int kSmem = kWindow ? C::kWindowSmemBytes : C::kSmemBytes;
-  if (!configure_kernel_smem(reinterpret_cast<const void*>(&paged_decode_kernel<D, FMT, L, kWindow>), kSmem)) return COOPT_ERR_CUDA;
-  return launch_dependent(paged_decode_kernel<D, FMT, L, kWindow>, grid, C::kThreads, kSmem, stream, p, table) ? COOPT_OK : COOPT_ERR_CUDA;
+  if (!configure_kernel_smem(reinterpret_cast<const void*>(&paged_decode_kernel<D, FMT, L, kWindow, 0>), kSmem)) return COOPT_ERR_CUDA;
+  return launch_dependent(paged_decode_kernel<D, FMT, L, kWindow, 0>, grid, C::kThreads, kSmem, stream, p, table) ? COOPT_OK : COOPT_ERR_CUDA;
+}
+// A windowed call whose units all have a CTA of their own at once, kPerSm of them on an SM, or a cluster of CTAs each: see
+// kFewPerSm in the kernel, and kFewBlocks.  `done` says whether it was one.
+template <int D, int FMT, int kPerSm>
+int launch_few(DecodeParams p, const LayerTable<1>& table, int listed_blocks, bool& done, cudaStream_t stream) {
+  using C = Cfg<D, FMT, kPerSm>;
+  const auto kernel = paged_decode_kernel<D, FMT, 1, true, kPerSm>;
+  const void* address = reinterpret_cast<const void*>(kernel);
+  const int units = p.batch * p.num_kv_heads;
+  const DeviceInfo* di = device_info();
+  if (di == nullptr) return COOPT_ERR_CUDA;
+  if (units > kPerSm * di->num_sms) return COOPT_OK;
+  if (!configure_kernel_smem(address, C::kWindowSmemBytes)) return COOPT_ERR_CUDA;
+  // as many CTAs as leave a block to a warp, where a warp would have more than one and a half and room is left
+  const int wanted = 2 * listed_blocks <= 3 * C::kWarps ? 1 : std::min(kMaxSplits, (listed_blocks + C::kWarps - 1) / C::kWarps);
+  p.splits = 0;
+  for (int s = wanted; s > 0 && p.splits == 0; --s)
+    if (units <= (s == 1 ? kPerSm * di->num_sms : clusters_at_once(address, s, C::kThreads, C::kWindowSmemBytes))) p.splits = s;
+  done = listed_blocks <= (C::kFp8 ? kFewBlocks : kFewBlocksBf16) * C::kWarps * p.splits;
+  if (!done) return COOPT_OK;
+  return launch_dependent_cluster(kernel, units * p.splits, p.splits, C::kThreads, C::kWindowSmemBytes, stream, p, table) ? COOPT_OK : COOPT_ERR_CUDA;
+}
+template <int D, int FMT>
+int launch_window(const DecodeParams& p, const LayerTable<1>& table, int grid, int listed_blocks, cudaStream_t stream) {
+  bool done = false;
+  int rc = launch_few<D, FMT, 1>(p, table, listed_blocks, done, stream);
+  if (!done && rc == COOPT_OK) rc = launch_few<D, FMT, 2>(p, table, listed_blocks, done, stream);
+  if (!done && rc == COOPT_OK) rc = launch_few<D, FMT, 3>(p, table, listed_blocks, done, stream);
+  return done || rc != COOPT_OK ? rc : launch_one<D, FMT, 1, true>(p, table, grid, stream);
 }
 
 // coopt_decode_plan: a copy of the step's context lengths and of the valid part of its block table, with the block ids
@@ -1198,7 +1318,11 @@ static int launch_layers(const DecodeParams& p, const coopt_layer_io* io, int gr
   }
   LayerTable<1> table;
   fill(table.l);
-  return p.window > 0 ? launch_one<D, FMT, 1, true>(p, table, grid, stream) : launch_one<D, FMT, 1, false>(p, table, grid, stream);
+  if (p.window > 0) {
+    const int listed = std::min(p.max_blocks_per_seq, sink_blocks(p.sinks) + p.window / kBlockSize + 2);    // most that a sequence lists
+    return launch_window<D, FMT>(p, table, grid, listed, stream);
+  }
+  return launch_one<D, FMT, 1, false>(p, table, grid, stream);
 }
 static int launch_attention(const DecodeParams& p, const coopt_layer_io* io, int head_dim, int dtype, int grid, cudaStream_t stream) {
   if (head_dim == 128) {

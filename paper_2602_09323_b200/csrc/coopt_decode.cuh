@@ -47,6 +47,11 @@ constexpr int kSoloUnits = 4;
 // (Four kv heads, eight layers / one, cut between warps and not: 160 sequences of 10 blocks 112 / 16.5 and 53 / 16.9 us, 400 of
 // 10 blocks 181 / 26.5 and 126 / 22.2, 400 of 1..16 blocks 175 / 25.8 and 112 / 30.0, 80 of 12 blocks 96 / 14.2 and 41 / 19.8.)
 constexpr int kSoloShare = 48, kSoloMost = 12;
+// Windowed calls: a unit keeps to its CTA (or cluster) as long as a warp gets no more than so many blocks of it, 20 us for a warp
+// alone on its SM (0.85 us a block, of a bf16 cache 0.55): the longest unit of many short ones is spread over no more warps.
+// (All units long: 50 sequences, 8 kv heads, head_dim 128, window 2048, 33 blocks a warp, 39.2 us so, 44.7 in a line; one of 4100
+// tokens among 143 of 100: 23.7, in a line 15.)
+constexpr int kFewBlocks = 24, kFewBlocksBf16 = 36;
 constexpr int kNoChunks = 1 << 30;    // "blocks per chunk" of a call without chunks
 
 // A plan: header, the clamped context lengths int32[batch] (padded to 16 bytes), the block table
@@ -113,6 +118,7 @@ struct DecodeParams {
   int solo_blocks;         // units of at most so many blocks are held whole by a warp
   int order;               // DecodeOrder
   float sm_scale_log2;     // sm_scale * log2(e)
+  int splits;              // windowed call of few units: CTAs (a cluster) that share one
   int window, sinks;       // windowed call: the last `window` tokens and the first `sinks` are seen; else unused
   int chunk_blocks;        // 0 = decode mode
   int max_chunks;

@@ -42,7 +42,6 @@
 // Every wait is bounded; a wait that runs out is reported in the status word and all roles leave through the common exit,
 // which frees the tensor memory.
 #include <algorithm>
-#include <mutex>
 
 #include "coopt_decode.cuh"
 #include "coopt_umma.cuh"
@@ -57,7 +56,6 @@ constexpr int kWidenWarp = 8, kMmaWarp = 12, kCopyWarp = 14;      // warp 15: sc
 constexpr int kTileBlocks = 8;
 constexpr int kTileKeys = kTileBlocks * kBlockSize;        // 128: what is copied and widened at a time
 constexpr int kHalf = kTileKeys / 2;                       // 64: what is multiplied at a time
-constexpr int kMaxSplits = 8;                              // CTAs of a cluster
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kMaxLag = 11.0f;                           // a row's reference may lag its maximum by this much (base-2 logarithm units)
 constexpr float kScaleLag = 16.0f;                         // a V scale may exceed the reference scale by this factor
@@ -149,28 +147,6 @@ __device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, volati
 }
 __device__ __forceinline__ void arrive_one(uint64_t* bar) {
   asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n @q mbarrier.arrive.shared::cta.b64 _, [%0];\n}" ::"r"(smem_u32(bar)) : "memory");
-}
-
-// All threads of the cluster's CTAs; what they have written to shared memory before is seen by all behind it.
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// Shared memory of CTA `rank` of the cluster, at the place that has address `addr` here.
-__device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, int rank) {
-  uint32_t a;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
-  return a;
-}
-__device__ __forceinline__ float2 ld_cluster_f2(uint32_t addr, int rank) {
-  float2 v;
-  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(cluster_addr(addr, rank)) : "memory");
-  return v;
-}
-__device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr, int rank) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(cluster_addr(addr, rank)) : "memory");
-  return v;
 }
 
 // kTurns: the two tiles of a CTA take turns at the exponentials.  A launch with one tile a CTA has a kernel without that code, which
@@ -912,35 +888,6 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
   if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
-// Clusters of that size that the device holds at a time; asked once.
-int clusters_at_once(const void* kernel, int size, int smem) {
-  static std::mutex mu;
-  static struct { const void* kernel; int dev, size, clusters; } known[512];
-  static int n = 0;
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return 0;
-  std::lock_guard<std::mutex> lock(mu);
-  for (int i = 0; i < n; ++i)
-    if (known[i].kernel == kernel && known[i].dev == dev && known[i].size == size) return known[i].clusters;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(size));
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = static_cast<size_t>(smem);
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = static_cast<unsigned>(size);
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  int clusters = 0;
-  if (cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) != cudaSuccess) {
-    (void)cudaGetLastError();
-    clusters = 0;
-  }
-  if (n < 512) known[n++] = {kernel, dev, size, clusters};
-  return clusters;
-}
-
 template <int D, bool kE5m2, bool kWindow>
 int launch_one(const coopt_cache* c, PrefillParams p, long long pairs, long long likely, long long key_tiles, cudaStream_t stream) {
   using C = Cfg<D>;
@@ -956,7 +903,7 @@ int launch_one(const coopt_cache* c, PrefillParams p, long long pairs, long long
     // 21.9 / 17.2, and 27.9 with three, which do not fit at once.  Two tiles of keys are not worth it: 10.6 / 10.9.)
     if (kWindow && p.tiles == 1 && key_tiles > 2)
       for (int s = static_cast<int>(std::min<long long>(key_tiles, kMaxSplits)); s > 1 && p.splits == 1; --s)
-        if (likely <= clusters_at_once(reinterpret_cast<const void*>(kernel), s, C::kSmemBytes)) p.splits = s;
+        if (likely <= clusters_at_once(reinterpret_cast<const void*>(kernel), s, kThreads, C::kSmemBytes)) p.splits = s;
     if (pairs * c->num_kv_heads * p.splits > 0x7fffffffll) return COOPT_ERR_UNSUPPORTED;
     const dim3 grid(static_cast<unsigned>(pairs * c->num_kv_heads * p.splits));
     return launch_dependent_cluster(kernel, grid, kWindow ? p.splits : 1, kThreads, C::kSmemBytes, stream, p, map_part, map_hdr) ? COOPT_OK : COOPT_ERR_CUDA;

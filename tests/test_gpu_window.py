@@ -137,13 +137,14 @@ def test_many_sequences():
 
 @pytest.mark.parametrize("fmt", ["e4m3", "e5m2", "bf16"])
 def test_a_window_over_everything_is_the_call_without_one(fmt):
+    # (both calls are held to the definition: what is joined in which order is each one's own)
     lens = [700, 1, 0, 33, 2000, 129]
-    w = workloads.make_workload("whole", lens, 10, 2, 128, seed=17)
-    cache = helpers.gpu_fill(w, FMT[fmt])
-    want, _ = helpers.gpu_decode(w, cache)
-    assert torch.equal(decode(w, cache, w.block_table, lens, 2000, 0), want)
+    w, cache, kv, table = make(lens, [1] * 6, 10, 2, 128, fmt, 2000, 0, seed=17, poison=False)
+    ref, spread = attention.window_attention(w.q.float().numpy(), kv, w.block_table.numpy(), lens, 2000, 0)
+    whole, _ = helpers.gpu_decode(w, cache)
+    for out in (whole, decode(w, cache, w.block_table, lens, 2000, 0)):
+        check(out, ref, spread, fmt)
     if fmt != "bf16":
-        # (runs of query tokens: keys may be shared out to several CTAs, so both calls are held to the definition)
         lens, q_lens = [700, 33, 300], [500, 2, 40]
         w, cache, kv, table = make(lens, q_lens, 10, 2, 128, fmt, 700, 0, seed=18, poison=False)
         ref, spread = attention.window_attention(w.q.float().numpy(), kv, w.block_table.numpy(), lens, 700, 0, w.cu_q_lens.numpy())
