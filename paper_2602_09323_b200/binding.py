@@ -420,8 +420,15 @@ def _need(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
-def _device() -> int:
-    return torch.cuda.current_device() if _current_device is None else _current_device()
+if _current_device is not None and _raw_stream is not None:
+    _device = _current_device                    # (the very functions: a wrapper around each costs as much again)
+    _stream_of = _raw_stream
+else:
+    def _device() -> int:
+        return torch.cuda.current_device()
+
+    def _stream_of(device: int) -> int:
+        return torch.cuda.current_stream(device).cuda_stream
 
 
 def _here(*tensors) -> None:
@@ -441,14 +448,6 @@ def _window_inputs(cache: Cache, q, block_table, context_lens, workspace, out, r
     _need(rows is None or rows == block_table.shape[0], "one query row per row of the table")
 
 
-def _window_ok(cache: Cache, q, table, lens, ws, out) -> bool:
-    device = _device()
-    return (q.get_device() == device and out.get_device() == device and table.get_device() == device and lens.get_device() == device
-            and ws.get_device() == device and cache.data.get_device() == device and q.dtype is _BF16 and out.dtype is _BF16 and table.dtype is _I32
-            and lens.dtype is _I32 and ws.dtype is _U8 and q.is_contiguous() and out.is_contiguous() and table.is_contiguous() and lens.is_contiguous()
-            and ws.is_contiguous())
-
-
 def window_decode(cache: Cache, q: torch.Tensor, block_table: torch.Tensor, context_lens: torch.Tensor, window: int, sinks: int,
                   sm_scale: float, workspace: torch.Tensor, k_new: Optional[torch.Tensor] = None, v_new: Optional[torch.Tensor] = None,
                   slot_mapping: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -456,9 +455,12 @@ def window_decode(cache: Cache, q: torch.Tensor, block_table: torch.Tensor, cont
     (bf16 [B, Hkv, D], token stride taken from the tensor) and slot_mapping (int64 [B]) the new tokens are written first."""
     if out is None:
         out = torch.empty_like(q)
-    shape, width = q.shape, block_table.shape
-    if not (_window_ok(cache, q, block_table, context_lens, workspace, out) and len(shape) == 3 and len(width) == 2 and shape[2] == cache.head_dim
-            and out.shape == shape and shape[0] == width[0] == context_lens.numel()):
+    device, shape, width = _device(), q.shape, block_table.shape
+    if not (q.get_device() == out.get_device() == block_table.get_device() == context_lens.get_device() == workspace.get_device()
+            == cache.data.get_device() == device and q.dtype is out.dtype is _BF16 and block_table.dtype is context_lens.dtype is _I32
+            and workspace.dtype is _U8 and q.is_contiguous() and out.is_contiguous() and block_table.is_contiguous() and context_lens.is_contiguous()
+            and workspace.is_contiguous() and len(shape) == 3 and len(width) == 2 and shape[2] == cache.head_dim and out.shape == shape
+            and shape[0] == width[0] == context_lens.numel()):
         _window_inputs(cache, q, block_table, context_lens, workspace, out, q.shape[0])
     stride, k, v, slots = 0, None, None, None
     if k_new is not None or v_new is not None or slot_mapping is not None:
@@ -472,9 +474,9 @@ def window_decode(cache: Cache, q: torch.Tensor, block_table: torch.Tensor, cont
         _here(k_new, v_new, slot_mapping)
         stride = at[0] if rows > 1 else heads * shape[2]
         k, v, slots = k_new.data_ptr(), v_new.data_ptr(), slot_mapping.data_ptr()
-    st = load_library().coopt_window_decode(cache._ref, k, v, stride, slots, q.data_ptr(), out.data_ptr(), block_table.data_ptr(), width[1],
+    st = (_lib or load_library()).coopt_window_decode(cache._ref, k, v, stride, slots, q.data_ptr(), out.data_ptr(), block_table.data_ptr(), width[1],
                                             context_lens.data_ptr(), shape[0], shape[1], window, sinks, sm_scale, workspace.data_ptr(),
-                                            workspace.numel(), _stream())
+                                            workspace.numel(), _stream_of(device))
     if st != 0:
         _check(st, "coopt_window_decode")
     return out
@@ -486,16 +488,18 @@ def window_prefill(cache: Cache, q: torch.Tensor, cu_q_lens: torch.Tensor, block
     ``sinks``; cu_q_lens int32 [B + 1] on the device.  Rows from cu_q_lens[B] on are left as they are."""
     if out is None:
         out = torch.empty_like(q)
-    shape, width = q.shape, block_table.shape
-    if not (_window_ok(cache, q, block_table, context_lens, workspace, out) and len(shape) == 3 and len(width) == 2 and shape[2] == cache.head_dim
-            and out.shape == shape and width[0] == context_lens.numel()):
+    device, shape, width = _device(), q.shape, block_table.shape
+    if not (q.get_device() == out.get_device() == block_table.get_device() == context_lens.get_device() == workspace.get_device()
+            == cache.data.get_device() == device and q.dtype is out.dtype is _BF16 and block_table.dtype is context_lens.dtype is _I32
+            and workspace.dtype is _U8 and q.is_contiguous() and out.is_contiguous() and block_table.is_contiguous() and context_lens.is_contiguous()
+            and workspace.is_contiguous() and len(shape) == 3 and len(width) == 2 and shape[2] == cache.head_dim and out.shape == shape
+            and width[0] == context_lens.numel()):
         _window_inputs(cache, q, block_table, context_lens, workspace, out, None)
-    if not (cu_q_lens.dtype is _I32 and cu_q_lens.is_contiguous() and cu_q_lens.numel() == width[0] + 1):
-        raise ValueError("cu_q_lens: contiguous int32 [B + 1]")
-    _here(cu_q_lens)
-    st = load_library().coopt_window_prefill(cache._ref, q.data_ptr(), out.data_ptr(), cu_q_lens.data_ptr(), block_table.data_ptr(), width[1],
+    if not (cu_q_lens.dtype is _I32 and cu_q_lens.is_contiguous() and cu_q_lens.numel() == width[0] + 1 and cu_q_lens.get_device() == device):
+        raise ValueError("cu_q_lens: contiguous int32 [B + 1] on the current CUDA device")
+    st = (_lib or load_library()).coopt_window_prefill(cache._ref, q.data_ptr(), out.data_ptr(), cu_q_lens.data_ptr(), block_table.data_ptr(), width[1],
                                              context_lens.data_ptr(), width[0], shape[1], shape[0], window, sinks, sm_scale,
-                                             workspace.data_ptr(), workspace.numel(), _stream())
+                                             workspace.data_ptr(), workspace.numel(), _stream_of(device))
     if st != 0:
         _check(st, "coopt_window_prefill")
     return out
@@ -567,7 +571,7 @@ def pages_copy(caches: CacheSet, src: torch.Tensor, dst: torch.Tensor) -> None:
     device = _device()
     n = _lists(device, src, dst)
     _need(caches.device == device, "caches: on the current CUDA device")
-    st = load_library().coopt_pages_copy(caches.array, len(caches.keep), src.data_ptr(), dst.data_ptr(), n, _stream())
+    st = (_lib or load_library()).coopt_pages_copy(caches.array, len(caches.keep), src.data_ptr(), dst.data_ptr(), n, _stream_of(device))
     if st != 0:
         _check(st, "coopt_pages_copy")
 
@@ -577,7 +581,7 @@ def pages_reserve(pages: Pages, row_ids: torch.Tensor, new_lens: torch.Tensor, w
     device = _device()
     n = _lists(device, row_ids, new_lens)
     _pool_here(device, pages, workspace)
-    st = load_library().coopt_pages_reserve(pages._ref, row_ids.data_ptr(), new_lens.data_ptr(), n, workspace.data_ptr(), workspace.numel(), _stream())
+    st = (_lib or load_library()).coopt_pages_reserve(pages._ref, row_ids.data_ptr(), new_lens.data_ptr(), n, workspace.data_ptr(), workspace.numel(), _stream_of(device))
     if st != 0:
         _check(st, "coopt_pages_reserve")
 
@@ -587,8 +591,8 @@ def pages_fork(caches: CacheSet, pages: Pages, parents: torch.Tensor, children: 
     device = _device()
     n = _lists(device, parents, children)
     _pool_here(device, pages, workspace, caches)
-    st = load_library().coopt_pages_fork(caches.array, len(caches.keep), pages._ref, parents.data_ptr(), children.data_ptr(), n,
-                                         workspace.data_ptr(), workspace.numel(), _stream())
+    st = (_lib or load_library()).coopt_pages_fork(caches.array, len(caches.keep), pages._ref, parents.data_ptr(), children.data_ptr(), n,
+                                         workspace.data_ptr(), workspace.numel(), _stream_of(device))
     if st != 0:
         _check(st, "coopt_pages_fork")
 
@@ -598,7 +602,7 @@ def pages_release(pages: Pages, row_ids: torch.Tensor, workspace: torch.Tensor, 
     device = _device()
     n = _lists(device, row_ids, row_ids)
     _pool_here(device, pages, workspace)
-    st = load_library().coopt_pages_release(pages._ref, row_ids.data_ptr(), n, window, sinks, workspace.data_ptr(), workspace.numel(), _stream())
+    st = (_lib or load_library()).coopt_pages_release(pages._ref, row_ids.data_ptr(), n, window, sinks, workspace.data_ptr(), workspace.numel(), _stream_of(device))
     if st != 0:
         _check(st, "coopt_pages_release")
 
@@ -617,8 +621,8 @@ def pages_compact(caches: CacheSet, pages: Pages, workspace: torch.Tensor, table
             and table_out.shape == pages.block_table.shape and refs_out.shape == pages.refs.shape and used_out.numel() == 1
             and table_out.get_device() == refs_out.get_device() == used_out.get_device() == device):
         raise ValueError("table_out, refs_out: like the pool's own; used_out: one int32; on the current CUDA device")
-    st = load_library().coopt_pages_compact(caches.array, len(caches.keep), pages._ref, table_out.data_ptr(), refs_out.data_ptr(), used_out.data_ptr(),
-                                            workspace.data_ptr(), workspace.numel(), _stream())
+    st = (_lib or load_library()).coopt_pages_compact(caches.array, len(caches.keep), pages._ref, table_out.data_ptr(), refs_out.data_ptr(), used_out.data_ptr(),
+                                            workspace.data_ptr(), workspace.numel(), _stream_of(device))
     if st != 0:
         _check(st, "coopt_pages_compact")
     return used_out

@@ -355,33 +355,49 @@ struct TableWork {
 // A warp copies a granule at a time, kDepth 16-byte pieces of a lane in flight: HBM bounds it (one read and one write of
 // what is copied), and with 32 warps an SM 128 KB are under way, more than the latency needs.
 constexpr int kDepth = 8;
+__device__ __forceinline__ void copy_granule(const Copies& c, uint8_t* cache, int from, int to, unsigned head, int lane) {
+  if (from < 0 || from >= c.blocks || to < 0 || to >= c.blocks) return;
+  const uint4* in = reinterpret_cast<const uint4*>(cache + (static_cast<size_t>(from) * c.heads + head) * c.granule);
+  uint4* out = reinterpret_cast<uint4*>(cache + (static_cast<size_t>(to) * c.heads + head) * c.granule);
+  const int n = c.bytes / 16;
+  for (int i0 = lane; i0 < n; i0 += 32 * kDepth) {
+    uint4 v[kDepth];
+#pragma unroll
+    for (int k = 0; k < kDepth; ++k)
+      if (i0 + 32 * k < n) v[k] = in[i0 + 32 * k];
+#pragma unroll
+    for (int k = 0; k < kDepth; ++k)
+      if (i0 + 32 * k < n) out[i0 + 32 * k] = v[k];
+  }
+}
 __device__ __forceinline__ void copy_granules(const Copies& c, int first_warp, int warps, int lane) {
   const int pairs = c.count != nullptr ? *c.count : c.pairs;
   const unsigned items = static_cast<unsigned>(pairs) * c.heads;
-  uint8_t* cache = c.cache[blockIdx.y];
   for (unsigned t = first_warp; t < items; t += warps) {
-    const unsigned pair = t / c.heads, head = t - pair * c.heads;
-    const int from = c.src[pair], to = c.dst[pair];
-    if (from < 0 || from >= c.blocks || to < 0 || to >= c.blocks) continue;
-    const uint4* in = reinterpret_cast<const uint4*>(cache + (static_cast<size_t>(from) * c.heads + head) * c.granule);
-    uint4* out = reinterpret_cast<uint4*>(cache + (static_cast<size_t>(to) * c.heads + head) * c.granule);
-    const int n = c.bytes / 16;
-    for (int i0 = lane; i0 < n; i0 += 32 * kDepth) {
-      uint4 v[kDepth];
-#pragma unroll
-      for (int k = 0; k < kDepth; ++k)
-        if (i0 + 32 * k < n) v[k] = in[i0 + 32 * k];
-#pragma unroll
-      for (int k = 0; k < kDepth; ++k)
-        if (i0 + 32 * k < n) out[i0 + 32 * k] = v[k];
-    }
+    const unsigned pair = t / c.heads;
+    copy_granule(c, c.cache[blockIdx.y], c.src[pair], c.dst[pair], t - pair * c.heads, lane);
   }
+}
+// A row of the table that a fork writes: entry j of a child whose parent holds `len` tokens.
+__device__ __forceinline__ void fork_entry(const Pool& pool, int* status, int parent, int child, int len, int tail_dst, int j) {
+  int id = -1;
+  if (j < len / kBlockSize) {
+    id = pool.table[static_cast<size_t>(parent) * pool.width + j];
+    if (id >= pool.blocks) {
+      report(status, COOPT_ERR_INVALID_ARG);
+      id = -1;
+    }
+    if (id >= 0) atomicAdd(&pool.refs[id], 1); else id = -1;
+  } else if (j * kBlockSize < len) {
+    id = tail_dst;
+  }
+  pool.table[static_cast<size_t>(child) * pool.width + j] = id;
 }
 
 template <Tables kTables>
 __global__ void __launch_bounds__(kCopyThreads) pages_move_kernel(const __grid_constant__ Copies c, const __grid_constant__ TableWork w) {
   wait_previous_kernel();
-  const int lane = threadIdx.x & 31, warp = (blockIdx.x * kCopyThreads + threadIdx.x) >> 5, warps = gridDim.x * (kCopyThreads / 32);
+  const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) * gridDim.x + blockIdx.x, warps = gridDim.x * (kCopyThreads / 32);
   if (kTables != kNoTables && blockIdx.y == 0) {
     const Pool& pool = w.pool;
     const int thread = blockIdx.x * kCopyThreads + threadIdx.x, threads = gridDim.x * kCopyThreads;
@@ -391,19 +407,7 @@ __global__ void __launch_bounds__(kCopyThreads) pages_move_kernel(const __grid_c
       for (long long t = warp; t < static_cast<long long>(w.forks) * per_row; t += warps) {
         const int i = static_cast<int>(t / per_row), j = static_cast<int>(t - static_cast<long long>(i) * per_row) * 32 + lane;
         const int len = w.plan.fork_len[i];
-        if (len < 0 || j >= pool.width) continue;
-        int id = -1;
-        if (j < len / kBlockSize) {
-          id = pool.table[static_cast<size_t>(w.parents[i]) * pool.width + j];
-          if (id >= pool.blocks) {
-            report(w.plan.status, COOPT_ERR_INVALID_ARG);
-            id = -1;
-          }
-          if (id >= 0) atomicAdd(&pool.refs[id], 1); else id = -1;
-        } else if (j * kBlockSize < len) {
-          id = w.plan.dst[i];
-        }
-        pool.table[static_cast<size_t>(w.children[i]) * pool.width + j] = id;
+        if (len >= 0 && j < pool.width) fork_entry(pool, w.plan.status, w.parents[i], w.children[i], len, w.plan.dst[i], j);
       }
     } else {
       const int U = w.plan.header[0];
@@ -424,6 +428,192 @@ __global__ void __launch_bounds__(kCopyThreads) pages_move_kernel(const __grid_c
     }
   }
   copy_granules(c, warp, warps, lane);
+}
+
+// ---- fork and compaction of smaller pools, in one launch ---------------------------------------------------------------------
+// Every CTA looks through the counts and makes the whole plan for itself, in shared memory, then does its part of the work: what a
+// second launch and the way of the plan through memory would take is saved.  Nothing that a CTA writes on its way changes
+// another one's plan: blocks that are in use stay so, parents are no children.  What would (the new blocks' counts and the
+// children's lengths; in place, the moved counts) is written by the CTA that has counted itself last, when all have made
+// their plans.
+constexpr int kOneThreads = 1024;
+constexpr int kOneBlocks = 1 << 15;
+constexpr int kOneForks = 1024;
+constexpr int kMaxOneSmem = 160 * 1024;
+static_assert((kMaxRows + kOneForks) * 4 + kOneBlocks / 8 <= kMaxOneSmem && (2 * (kOneBlocks / 32) + 2 * (kOneBlocks / 2 + 1)) * 4 <= kMaxOneSmem, "shared memory");
+int* one_counter(void* workspace) { return reinterpret_cast<int*>(static_cast<uint8_t*>(workspace) + kWsHeaderBytes); }
+
+struct OneSlice {
+  unsigned* bits;          // [blocks / 32]: used
+  int words, per_thread;
+  int before, used;        // as in Slice
+};
+__device__ __forceinline__ void load_pool(const Pool& pool, unsigned* bits, int* warp_sums, OneSlice& s) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  s.bits = bits;
+  s.words = (pool.blocks + 31) / 32;
+  s.per_thread = (s.words + kOneThreads - 1) / kOneThreads;
+  constexpr int kUnroll = 8;
+  for (int w0 = warp * kUnroll; w0 < s.words; w0 += kOneThreads / 32 * kUnroll) {
+    int r[kUnroll];
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) {
+      const int id = (w0 + k) * 32 + lane;
+      r[k] = id < pool.blocks ? __ldcg(pool.refs + id) : 0;
+    }
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) {
+      const unsigned b = __ballot_sync(0xffffffffu, r[k] > 0);
+      if (lane == 0 && w0 + k < s.words) bits[w0 + k] = b;
+    }
+  }
+  __syncthreads();
+  int n = 0;
+  for (int w = threadIdx.x * s.per_thread; w < min(s.words, (static_cast<int>(threadIdx.x) + 1) * s.per_thread); ++w) n += __popc(bits[w]);
+  s.before = cta_scan(n, warp_sums, s.used);
+}
+// By all threads, behind the last read that a plan is made of: whether this CTA is the last to get here.
+__device__ __forceinline__ bool last_to_plan(int* counter, int* flag) {
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    int old;
+    asm volatile("atom.add.acq_rel.gpu.s32 %0, [%1], 1;" : "=r"(old) : "l"(counter) : "memory");
+    *flag = old == static_cast<int>(gridDim.x) - 1;
+    if (*flag) *counter = 0;             // ready for the next call
+  }
+  __syncthreads();
+  return *flag != 0;
+}
+
+__global__ void __launch_bounds__(kOneThreads, 1) pages_fork_one_kernel(const __grid_constant__ Copies c, int layers, const Pool pool, int* status, int* counter,
+                                                                        const int* parents, const int* children, int n) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ int warp_sums[32], flag;
+  __shared__ int src[kOneForks], dst[kOneForks], lens[kOneForks];
+  wait_previous_kernel();
+  int* owner = reinterpret_cast<int*>(smem);
+  int* list = owner + pool.rows;
+  unsigned* bits = reinterpret_cast<unsigned*>(list + n);
+  const int i = threadIdx.x, lane = threadIdx.x & 31;
+  static_assert(kOneThreads == kOneForks, "a fork to a thread");
+  const int p = i < n ? parents[i] : -1, child = i < n ? children[i] : -1;
+  const bool rows_ok = p >= 0 && p < pool.rows && child >= 0 && child < pool.rows;
+  const int L = rows_ok ? max(0, min(__ldcg(pool.lens + p), pool.width * kBlockSize)) : 0, old_len = rows_ok ? __ldcg(pool.lens + child) : 1;
+  for (int r = threadIdx.x; r < pool.rows; r += kOneThreads) owner[r] = INT_MAX;
+  int tail = L % kBlockSize != 0 ? pool.table[static_cast<size_t>(p) * pool.width + L / kBlockSize] : -1;
+  if (tail >= pool.blocks) tail = -1;
+  OneSlice s;
+  load_pool(pool, bits, warp_sums, s);
+  if (i < n && child >= 0 && child < pool.rows) atomicMin(&owner[child], i);
+  __syncthreads();
+  // a child is an empty row, named once, and no parent of another
+  const bool ok = rows_ok && owner[child] == i && owner[p] == INT_MAX && old_len == 0;
+  if (i < n && !ok && blockIdx.x == 0) report(status, COOPT_ERR_INVALID_ARG);
+  const bool copy = ok && tail >= 0;
+  int total;
+  const int rank = cta_scan(copy ? 1 : 0, warp_sums, total), free_blocks = pool.blocks - s.used;
+  {
+    int used = s.before;
+    for (int w = threadIdx.x * s.per_thread; w < min(s.words, (static_cast<int>(threadIdx.x) + 1) * s.per_thread); ++w) {
+      unsigned free_bits = ~bits[w];
+      if (32 * w + 32 > pool.blocks) free_bits &= (1u << (pool.blocks - 32 * w)) - 1u;
+      int k = 32 * w - used;
+      used += __popc(bits[w]);
+      for (; free_bits != 0 && k < total; free_bits &= free_bits - 1, ++k) list[k] = 32 * w + __ffs(free_bits) - 1;
+    }
+  }
+  const bool last = last_to_plan(counter, &flag);
+  const bool refused = !ok || (copy && rank >= free_blocks);
+  if (i < n) {
+    src[i] = refused ? -1 : tail;
+    dst[i] = copy && !refused ? list[rank] : -1;
+    lens[i] = refused ? -1 : L;
+    if (ok && refused && blockIdx.x == 0) report(status, COOPT_ERR_PAGES);
+    if (last && !refused) {
+      if (copy) pool.refs[dst[i]] = 1;
+      if (L > 0) pool.lens[child] = L;
+    }
+  }
+  __syncthreads();
+  const int warp = (threadIdx.x >> 5) * gridDim.x + blockIdx.x, warps = gridDim.x * (kOneThreads / 32);     // (few granules: on all SMs)
+  const int per_row = (pool.width + 31) / 32;
+  for (int t = warp; t < n * per_row; t += warps) {
+    const int f = t / per_row, j = (t - f * per_row) * 32 + lane;
+    if (lens[f] >= 0 && j < pool.width) fork_entry(pool, status, parents[f], children[f], lens[f], dst[f], j);
+  }
+  const unsigned granules = static_cast<unsigned>(n) * c.heads, items = granules * layers;
+  for (unsigned t = warp; t < items; t += warps) {
+    const unsigned y = t / granules, at = t - y * granules, f = at / c.heads;
+    copy_granule(c, c.cache[y], src[f], dst[f], at - f * c.heads, lane);
+  }
+}
+
+__global__ void __launch_bounds__(kOneThreads, 1) pages_compact_one_kernel(const __grid_constant__ Copies c, int layers, const Pool pool, int* status, int* counter,
+                                                                           int* table_out, int* refs_out, int* used_out) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ int warp_sums[32], flag;
+  wait_previous_kernel();
+  unsigned* bits = reinterpret_cast<unsigned*>(smem);
+  OneSlice s;
+  load_pool(pool, bits, warp_sums, s);
+  int* before = reinterpret_cast<int*>(bits + s.words);      // used blocks ahead of every word
+  int* holes = before + s.words;                             // [blocks / 2 + 1] each
+  int* movers = holes + pool.blocks / 2 + 1;
+  const int U = s.used, lane = threadIdx.x & 31;
+  const int w0 = threadIdx.x * s.per_thread, w1 = min(s.words, w0 + s.per_thread);
+  auto below = [&](int id0) { return id0 + 32 <= U ? 0xFFFFFFFFu : id0 >= U ? 0u : (1u << (U - id0)) - 1u; };
+  int n = 0, stay;                                           // used blocks below U
+  for (int w = w0; w < w1; ++w) n += __popc(bits[w] & below(32 * w));
+  cta_scan(n, warp_sums, stay);
+  int used = s.before;
+  for (int w = w0; w < w1; ++w) {
+    const int id0 = 32 * w;
+    const unsigned b = bits[w], low = below(id0);
+    before[w] = used;
+    int hole = id0 - used, mover = used - stay;
+    if (low != 0xFFFFFFFFu) mover += __popc(b & low);
+    for (unsigned f = ~b & low; f != 0; f &= f - 1, ++hole) holes[hole] = id0 + __ffs(f) - 1;
+    for (unsigned m = b & ~low; m != 0; m &= m - 1, ++mover) movers[mover] = id0 + __ffs(m) - 1;
+    used += __popc(b);
+  }
+  const int moves = U - stay;
+  const bool in_place = refs_out == pool.refs;
+  if (last_to_plan(counter, &flag)) {
+    if (in_place)
+      for (int i = threadIdx.x; i < moves; i += kOneThreads) {
+        refs_out[holes[i]] = __ldcg(pool.refs + movers[i]);
+        refs_out[movers[i]] = 0;
+      }
+    if (threadIdx.x == 0) *used_out = U;
+  }
+  // the number of a block from now on, -1 if it is free
+  auto goes = [&](int id) {
+    const unsigned b = bits[id >> 5], bit = 1u << (id & 31);
+    if ((b & bit) == 0) return -1;
+    return id < U ? id : holes[before[id >> 5] + __popc(b & (bit - 1u)) - stay];
+  };
+  const int thread = blockIdx.x * kOneThreads + threadIdx.x, threads = gridDim.x * kOneThreads;
+  if (!in_place) {
+    for (int id = thread; id < pool.blocks; id += threads) {
+      const int to = goes(id);
+      if (to >= 0) refs_out[to] = pool.refs[id];
+      if (id >= U) refs_out[id] = 0;                         // (a hole below U gets its mover's count)
+    }
+  }
+  const long long entries = static_cast<long long>(pool.rows) * pool.width;
+  for (long long e = thread; e < entries; e += threads) {
+    int id = pool.table[e];
+    if (id >= 0) {
+      id = id < pool.blocks ? goes(id) : -1;
+      if (id < 0) report(status, COOPT_ERR_INVALID_ARG);
+    }
+    table_out[e] = id;
+  }
+  const unsigned granules = static_cast<unsigned>(moves) * c.heads, items = granules * layers;
+  for (unsigned t = (threadIdx.x >> 5) * gridDim.x + blockIdx.x; t < items; t += threads >> 5) {
+    const unsigned y = t / granules, at = t - y * granules, i = at / c.heads;
+    copy_granule(c, c.cache[y], movers[i], holes[i], at - i * c.heads, lane);
+  }
 }
 
 // ---- release ----------------------------------------------------------------------------------------------------------
@@ -493,6 +683,19 @@ int launch_plan(Kernel* kernel, int smem, cudaStream_t stream, const Args&... ar
   if (!configure_kernel_smem(reinterpret_cast<const void*>(kernel), kMaxPlanSmem)) return COOPT_ERR_CUDA;
   return launch_dependent(kernel, kClusterCtas, kPlanThreads, smem, stream, args...) ? COOPT_OK : COOPT_ERR_CUDA;
 }
+void describe(const coopt_cache* caches, int layers, Copies& c) {
+  const coopt_cache& k = caches[0];
+  c.blocks = k.num_blocks;
+  c.heads = k.num_kv_heads;
+  c.granule = granule_bytes(k.head_dim, is_fp8(k.dtype));
+  c.bytes = is_fp8(k.dtype) ? header_offset(k.head_dim) + kFp8Header : c.granule;
+  for (int y = 0; y < layers; ++y) c.cache[y] = static_cast<uint8_t*>(caches[y].data);
+}
+// CTAs of a launch that plans in every one: a warp to eight granules, or entries of tables, and no more than there are SMs.
+int one_grid(long long granules, long long entries, int num_sms) {
+  const long long work = (granules > entries / 32 ? granules : entries / 32) / 8 + 1;
+  return static_cast<int>(work < num_sms ? work : num_sms);
+}
 // `most`: pairs there can be at most; `entries`: of tables and counts, for the first launch.
 template <Tables kTables>
 int launch_move(const coopt_cache* caches, int num_caches, Copies c, const TableWork& w, long long most, long long entries, cudaStream_t stream) {
@@ -502,12 +705,7 @@ int launch_move(const coopt_cache* caches, int num_caches, Copies c, const Table
   do {
     const int layers = num_caches - done < kCachesPerLaunch ? num_caches - done : kCachesPerLaunch;
     if (layers > 0) {
-      const coopt_cache& k = caches[0];
-      c.blocks = k.num_blocks;
-      c.heads = k.num_kv_heads;
-      c.granule = granule_bytes(k.head_dim, is_fp8(k.dtype));
-      c.bytes = is_fp8(k.dtype) ? header_offset(k.head_dim) + kFp8Header : c.granule;
-      for (int y = 0; y < layers; ++y) c.cache[y] = static_cast<uint8_t*>(caches[done + y].data);
+      describe(caches + done, layers, c);
     } else {
       c.pairs = 0;
       c.count = nullptr;
@@ -576,10 +774,25 @@ int coopt_pages_fork(const coopt_cache* caches, int32_t num_caches, const coopt_
   if (num_forks == 0) return COOPT_OK;
   if (!parents || !children) return COOPT_ERR_INVALID_ARG;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const DeviceInfo* di = device_info();
+  if (di == nullptr) return COOPT_ERR_CUDA;
+  Copies c = {};
+  const long long row_entries = static_cast<long long>(num_forks) * pages->max_blocks_per_seq;
+  if (pages->num_blocks <= kOneBlocks && num_forks <= kOneForks && num_caches <= kCachesPerLaunch && row_entries < (1ll << 30) &&
+      static_cast<long long>(num_forks) * num_caches * (num_caches > 0 ? caches[0].num_kv_heads : 1) < (1ll << 31)) {
+    if (num_caches > 0) describe(caches, num_caches, c); else c.heads = 1;
+    const int smem = (pages->rows + num_forks) * 4 + (pages->num_blocks + 31) / 32 * 4;
+    if (!configure_kernel_smem(reinterpret_cast<const void*>(&pages_fork_one_kernel), kMaxOneSmem)) return COOPT_ERR_CUDA;
+    const int grid = one_grid(static_cast<long long>(num_forks) * num_caches * c.heads, row_entries, di->num_sms);
+    return launch_dependent(pages_fork_one_kernel, grid, kOneThreads, smem, st, c, static_cast<int>(num_caches), pool_of(pages), static_cast<int*>(workspace),
+                            one_counter(workspace), parents, children, static_cast<int>(num_forks))
+               ? COOPT_OK
+               : COOPT_ERR_CUDA;
+  }
   const Plan plan = plan_of(workspace, pages->num_blocks, pages->rows);
   rc = launch_plan(&pages_fork_plan_kernel, plan_smem(pages, num_forks), st, pool_of(pages), plan, parents, children, static_cast<int>(num_forks));
   if (rc != COOPT_OK) return rc;
-  Copies c = {};
+  c = {};
   c.src = plan.src;
   c.dst = plan.dst;
   c.pairs = num_forks;
@@ -611,15 +824,29 @@ int coopt_pages_compact(const coopt_cache* caches, int32_t num_caches, const coo
   if (rc != COOPT_OK) return rc;
   if (!table_out || !refs_out || !used_out) return COOPT_ERR_INVALID_ARG;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const long long entries = static_cast<long long>(pages->rows) * pages->max_blocks_per_seq;
+  const DeviceInfo* di = device_info();
+  if (di == nullptr) return COOPT_ERR_CUDA;
+  Copies c = {};
+  if (pages->num_blocks <= kOneBlocks && num_caches <= kCachesPerLaunch &&
+      static_cast<long long>(pages->num_blocks) * num_caches * (num_caches > 0 ? caches[0].num_kv_heads : 1) < (1ll << 31)) {
+    if (num_caches > 0) describe(caches, num_caches, c); else c.heads = 1;
+    const int words = (pages->num_blocks + 31) / 32, smem = (2 * words + 2 * (pages->num_blocks / 2 + 1)) * 4;
+    if (!configure_kernel_smem(reinterpret_cast<const void*>(&pages_compact_one_kernel), kMaxOneSmem)) return COOPT_ERR_CUDA;
+    const int grid = one_grid(static_cast<long long>(pages->num_blocks / 2) * num_caches * c.heads, entries, di->num_sms);
+    return launch_dependent(pages_compact_one_kernel, grid, kOneThreads, smem, st, c, static_cast<int>(num_caches), pool_of(pages), static_cast<int*>(workspace),
+                            one_counter(workspace), static_cast<int*>(table_out), static_cast<int*>(refs_out), static_cast<int*>(used_out))
+               ? COOPT_OK
+               : COOPT_ERR_CUDA;
+  }
   const Plan plan = plan_of(workspace, pages->num_blocks, pages->rows);
   rc = launch_plan(&pages_compact_plan_kernel, plan_smem(pages, 0), st, pool_of(pages), plan, static_cast<int*>(used_out));
   if (rc != COOPT_OK) return rc;
-  Copies c = {};
+  c = {};
   c.src = plan.src;
   c.dst = plan.dst;
   c.count = plan.header + 1;
   const TableWork w = {pool_of(pages), plan, nullptr, nullptr, 0, table_out, refs_out};
-  const long long entries = static_cast<long long>(pages->rows) * pages->max_blocks_per_seq;
   return launch_move<kCompactTables>(caches, num_caches, c, w, pages->num_blocks / 2 + 1, entries > pages->num_blocks ? entries : pages->num_blocks, st);
 }
 

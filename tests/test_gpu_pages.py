@@ -68,12 +68,18 @@ class Both:
         assert int(used.item()) == self.ref.compact()
 
 
-@pytest.mark.parametrize("dtype,dim,hkv,layers", [(binding.KV_FP8_E4M3, 64, 2, 2), (binding.KV_FP8_E5M2, 128, 1, 3), (binding.KV_BF16, 64, 3, 1),
-                                                  (binding.KV_BF16, 128, 2, 2), (binding.KV_FP8_E4M3, 128, 5, 1)])
-def test_a_run_of_calls(dtype, dim, hkv, layers):
+@pytest.mark.parametrize("dtype,dim,hkv,layers,blocks,steps", [(binding.KV_FP8_E4M3, 64, 2, 2, 67, 60), (binding.KV_FP8_E5M2, 128, 1, 3, 67, 60),
+                                                               (binding.KV_BF16, 64, 3, 1, 67, 60), (binding.KV_BF16, 128, 2, 2, 67, 60),
+                                                               (binding.KV_FP8_E4M3, 128, 5, 1, 67, 60), (binding.KV_FP8_E4M3, 64, 1, 1, 33000, 20),
+                                                               (binding.KV_FP8_E4M3, 64, 1, 67, 67, 30)])
+def test_a_run_of_calls(dtype, dim, hkv, layers, blocks, steps):
     rng = np.random.default_rng(dim + hkv)
-    p = Both(67, 14, 9, layers, hkv, dim, dtype, seed=1)
-    for step in range(60):
+    p = Both(blocks, 14, 9, layers, hkv, dim, dtype, seed=1)
+    if blocks > 1000:                                     # most of a large pool is held by others, the lowest free blocks lie far up
+        p.ref.refs[:blocks - 80] = 1
+        p.ref.refs[rng.choice(blocks, 30, replace=False)] = 0
+        p.pages.refs.copy_(torch.from_numpy(p.ref.refs))
+    for step in range(steps):
         kind = rng.choice(["reserve", "fork", "release", "trim", "compact"], p=[0.4, 0.25, 0.15, 0.12, 0.08])
         n = int(rng.integers(1, 6))
         if kind == "reserve":
