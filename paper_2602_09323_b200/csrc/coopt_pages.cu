@@ -354,7 +354,9 @@ struct TableWork {
 
 // A warp copies a granule at a time, kDepth 16-byte pieces of a lane in flight: HBM bounds it (one read and one write of
 // what is copied), and with 32 warps an SM 128 KB are under way, more than the latency needs.
-constexpr int kDepth = 8;
+// (Nine: the 258 pieces of a granule at head_dim 128 are on their way at once.  With eight and a second round for two of them
+// 700 blocks of 16 layers took 124 us.)
+constexpr int kDepth = 9;
 __device__ __forceinline__ void copy_granule(const Copies& c, uint8_t* cache, int from, int to, unsigned head, int lane) {
   if (from < 0 || from >= c.blocks || to < 0 || to >= c.blocks) return;
   const uint4* in = reinterpret_cast<const uint4*>(cache + (static_cast<size_t>(from) * c.heads + head) * c.granule);
@@ -370,9 +372,14 @@ __device__ __forceinline__ void copy_granule(const Copies& c, uint8_t* cache, in
       if (i0 + 32 * k < n) out[i0 + 32 * k] = v[k];
   }
 }
-__device__ __forceinline__ void copy_granules(const Copies& c, int first_warp, int warps, int lane) {
+// A warp's place among all: neighbours in a CTA, which copy neighbouring granules, or (few granules) spread over the SMs.
+__device__ __forceinline__ unsigned place_of_warp(unsigned items, int warps) {
+  const unsigned in_cta = blockDim.x >> 5, warp = threadIdx.x >> 5;
+  return items >= static_cast<unsigned>(warps) ? blockIdx.x * in_cta + warp : warp * gridDim.x + blockIdx.x;
+}
+__device__ __forceinline__ void copy_granules(const Copies& c, int warps, int lane) {
   const int pairs = c.count != nullptr ? *c.count : c.pairs;
-  const unsigned items = static_cast<unsigned>(pairs) * c.heads;
+  const unsigned items = static_cast<unsigned>(pairs) * c.heads, first_warp = place_of_warp(items, warps);
   for (unsigned t = first_warp; t < items; t += warps) {
     const unsigned pair = t / c.heads;
     copy_granule(c, c.cache[blockIdx.y], c.src[pair], c.dst[pair], t - pair * c.heads, lane);
@@ -427,7 +434,7 @@ __global__ void __launch_bounds__(kCopyThreads) pages_move_kernel(const __grid_c
       }
     }
   }
-  copy_granules(c, warp, warps, lane);
+  copy_granules(c, warps, lane);
 }
 
 // ---- fork and compaction of smaller pools, in one launch ---------------------------------------------------------------------
@@ -436,11 +443,15 @@ __global__ void __launch_bounds__(kCopyThreads) pages_move_kernel(const __grid_c
 // another one's plan: blocks that are in use stay so, parents are no children.  What would (the new blocks' counts and the
 // children's lengths; in place, the moved counts) is written by the CTA that has counted itself last, when all have made
 // their plans.
+// (us with a planning launch / so; release and fork of 8 rows over four layers, pool of 700 / 8000 / 30000 blocks 10.0 / 7.2, 9.9 /
+// 7.4, 10.3 / 9.5; compaction of two layers, 900 / 8000 / 30000 8.4 / 5.7, 11.0 / 9.1, 25.0 / 25.4; reserve by a cluster / by one
+// CTA, 700 / 16000 / 30000 6.5 / 4.4, 6.8 / 5.2, 6.5 / 6.6.)
 constexpr int kOneThreads = 1024;
 constexpr int kOneBlocks = 1 << 15;
-constexpr int kOneForks = 1024;
-constexpr int kMaxOneSmem = 160 * 1024;
-static_assert((kMaxRows + kOneForks) * 4 + kOneBlocks / 8 <= kMaxOneSmem && (2 * (kOneBlocks / 32) + 2 * (kOneBlocks / 2 + 1)) * 4 <= kMaxOneSmem, "shared memory");
+constexpr int kOneReserve = 1 << 14;
+constexpr int kOneForks = 1024;              // forks, or rows, of a call
+constexpr int kMaxOneSmem = 180 * 1024;
+static_assert((kMaxRows + kOneForks) * 4 + kOneBlocks / 8 <= kMaxOneSmem && kMaxRows * 4 + kOneBlocks / 8 + kOneBlocks * 4 <= kMaxOneSmem && (2 * (kOneBlocks / 32) + 2 * (kOneBlocks / 2 + 1)) * 4 <= kMaxOneSmem, "shared memory");
 int* one_counter(void* workspace) { return reinterpret_cast<int*>(static_cast<uint8_t*>(workspace) + kWsHeaderBytes); }
 
 struct OneSlice {
@@ -453,18 +464,19 @@ __device__ __forceinline__ void load_pool(const Pool& pool, unsigned* bits, int*
   s.bits = bits;
   s.words = (pool.blocks + 31) / 32;
   s.per_thread = (s.words + kOneThreads - 1) / kOneThreads;
-  constexpr int kUnroll = 8;
-  for (int w0 = warp * kUnroll; w0 < s.words; w0 += kOneThreads / 32 * kUnroll) {
+  constexpr int kUnroll = 8, kWarps = kOneThreads / 32;
+  for (int w0 = warp; w0 < s.words; w0 += kWarps * kUnroll) {
     int r[kUnroll];
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k) {
-      const int id = (w0 + k) * 32 + lane;
+      const int id = (w0 + k * kWarps) * 32 + lane;
       r[k] = id < pool.blocks ? __ldcg(pool.refs + id) : 0;
     }
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k) {
+      if (w0 + k * kWarps >= s.words) break;
       const unsigned b = __ballot_sync(0xffffffffu, r[k] > 0);
-      if (lane == 0 && w0 + k < s.words) bits[w0 + k] = b;
+      if (lane == 0) bits[w0 + k * kWarps] = b;
     }
   }
   __syncthreads();
@@ -542,7 +554,7 @@ __global__ void __launch_bounds__(kOneThreads, 1) pages_fork_one_kernel(const __
     if (lens[f] >= 0 && j < pool.width) fork_entry(pool, status, parents[f], children[f], lens[f], dst[f], j);
   }
   const unsigned granules = static_cast<unsigned>(n) * c.heads, items = granules * layers;
-  for (unsigned t = warp; t < items; t += warps) {
+  for (unsigned t = place_of_warp(items, warps); t < items; t += warps) {
     const unsigned y = t / granules, at = t - y * granules, f = at / c.heads;
     copy_granule(c, c.cache[y], src[f], dst[f], at - f * c.heads, lane);
   }
@@ -610,9 +622,95 @@ __global__ void __launch_bounds__(kOneThreads, 1) pages_compact_one_kernel(const
     table_out[e] = id;
   }
   const unsigned granules = static_cast<unsigned>(moves) * c.heads, items = granules * layers;
-  for (unsigned t = (threadIdx.x >> 5) * gridDim.x + blockIdx.x; t < items; t += threads >> 5) {
+  for (unsigned t = place_of_warp(items, threads >> 5); t < items; t += threads >> 5) {
     const unsigned y = t / granules, at = t - y * granules, i = at / c.heads;
     copy_granule(c, c.cache[y], movers[i], holes[i], at - i * c.heads, lane);
+  }
+}
+
+// Reserve, by one CTA: all that it does after the look through the counts is a trip to memory or two for every 128 rows.
+__global__ void __launch_bounds__(kOneThreads, 1) pages_reserve_one_kernel(const Pool pool, int* status, const int* row_ids, const int* new_lens, int n) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ int warp_sums[32];
+  __shared__ int rows[kOneForks], begin[kOneForks], end[kOneForks], need[kOneForks];
+  __shared__ unsigned first[kOneForks];            // which of a row's first 32 entries lack a block
+  wait_previous_kernel();
+  int* owner = reinterpret_cast<int*>(smem);
+  unsigned* bits = reinterpret_cast<unsigned*>(owner + pool.rows);
+  int* list = reinterpret_cast<int*>(bits + (pool.blocks + 31) / 32);
+  const int i = threadIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int row = i < n ? row_ids[i] : -1, to = i < n ? new_lens[i] : 0;
+  const bool row_ok = row >= 0 && row < pool.rows;
+  const int len = row_ok ? max(0, min(pool.lens[row], pool.width * kBlockSize)) : 0;
+  for (int r = threadIdx.x; r < pool.rows; r += kOneThreads) owner[r] = INT_MAX;
+  OneSlice s;
+  load_pool(pool, bits, warp_sums, s);
+  if (row_ok) atomicMin(&owner[row], i);
+  __syncthreads();
+  const bool ok = row_ok && owner[row] == i && to >= len && to <= pool.width * kBlockSize;
+  if (i < n) {
+    if (!ok) report(status, COOPT_ERR_INVALID_ARG);
+    rows[i] = row;
+    begin[i] = ok ? (len + kBlockSize - 1) / kBlockSize : 0;
+    end[i] = ok ? (to + kBlockSize - 1) / kBlockSize : 0;
+  }
+  __syncthreads();
+  // entries without a block: a warp to a row, four rows on their way at a time
+  constexpr int kRowsAt = 4, kWarps = kOneThreads / 32;
+  for (int f0 = warp; f0 < n; f0 += kRowsAt * kWarps) {
+    bool lacks[kRowsAt];
+#pragma unroll
+    for (int k = 0; k < kRowsAt; ++k) {
+      const int f = f0 + k * kWarps, j = f < n ? begin[f] + lane : 0;
+      lacks[k] = f < n && j < end[f] && pool.table[static_cast<size_t>(rows[f]) * pool.width + j] < 0;
+    }
+#pragma unroll
+    for (int k = 0; k < kRowsAt; ++k) {
+      const int f = f0 + k * kWarps;
+      if (f >= n) break;
+      const unsigned mask = __ballot_sync(0xffffffffu, lacks[k]);
+      int more = 0;
+      for (int j = begin[f] + 32 + lane; j < end[f]; j += 32) more += pool.table[static_cast<size_t>(rows[f]) * pool.width + j] < 0;
+      more = __reduce_add_sync(0xffffffffu, more);
+      if (lane == 0) { first[f] = mask; need[f] = more + __popc(mask); }
+    }
+  }
+  __syncthreads();
+  const int wants = i < n && ok ? need[i] : 0;
+  int total;
+  static_assert(INT_MAX / kOneThreads > kOneBlocks, "a sum that is cut short is still more than there is");
+  const int from = cta_scan(min(wants, INT_MAX / kOneThreads), warp_sums, total), free_blocks = pool.blocks - s.used;
+  const bool fits = wants == 0 || (wants <= free_blocks && from <= free_blocks - wants);
+  if (i < n) {
+    if (ok && !fits) report(status, COOPT_ERR_PAGES);
+    need[i] = ok && fits ? from : -1;
+  }
+  {
+    const int most = min(total, free_blocks);
+    int used = s.before;
+    for (int w = threadIdx.x * s.per_thread; w < min(s.words, (static_cast<int>(threadIdx.x) + 1) * s.per_thread); ++w) {
+      unsigned free_bits = ~bits[w];
+      if (32 * w + 32 > pool.blocks) free_bits &= (1u << (pool.blocks - 32 * w)) - 1u;
+      int k = 32 * w - used;
+      used += __popc(bits[w]);
+      for (; free_bits != 0 && k < most; free_bits &= free_bits - 1, ++k) list[k] = 32 * w + __ffs(free_bits) - 1;
+    }
+  }
+  __syncthreads();
+  if (ok && fits) pool.lens[row] = to;
+  for (int f = warp; f < n; f += kWarps) {
+    int at = need[f];
+    if (at < 0) continue;
+    int* entries = pool.table + static_cast<size_t>(rows[f]) * pool.width;
+    for (int j0 = begin[f]; j0 < end[f]; j0 += 32) {
+      const unsigned all = j0 == begin[f] ? first[f] : __ballot_sync(0xffffffffu, j0 + lane < end[f] && entries[j0 + lane] < 0);
+      if ((all >> lane) & 1u) {
+        const int id = list[at + __popc(all & ((1u << lane) - 1u))];
+        entries[j0 + lane] = id;
+        pool.refs[id] = 1;
+      }
+      at += __popc(all);
+    }
   }
 }
 
@@ -760,6 +858,14 @@ int coopt_pages_reserve(const coopt_pages* pages, const int32_t* row_ids, const 
   if (num_rows < 0 || num_rows > pages->rows) return COOPT_ERR_INVALID_ARG;
   if (num_rows == 0) return COOPT_OK;
   if (!row_ids || !new_lens) return COOPT_ERR_INVALID_ARG;
+  if (pages->num_blocks <= kOneReserve && num_rows <= kOneForks) {
+    if (!configure_kernel_smem(reinterpret_cast<const void*>(&pages_reserve_one_kernel), kMaxOneSmem)) return COOPT_ERR_CUDA;
+    const int smem = pages->rows * 4 + (pages->num_blocks + 31) / 32 * 4 + pages->num_blocks * 4;
+    return launch_dependent(pages_reserve_one_kernel, 1, kOneThreads, smem, static_cast<cudaStream_t>(stream), pool_of(pages), static_cast<int*>(workspace), row_ids,
+                            new_lens, static_cast<int>(num_rows))
+               ? COOPT_OK
+               : COOPT_ERR_CUDA;
+  }
   return launch_plan(&pages_reserve_kernel, plan_smem(pages, num_rows), static_cast<cudaStream_t>(stream), pool_of(pages),
                      plan_of(workspace, pages->num_blocks, pages->rows), row_ids, new_lens, static_cast<int>(num_rows));
 }
