@@ -345,9 +345,10 @@ int coopt_window_prefill(const coopt_cache* cache, const void* q, void* out, con
 /*
  * Pages: the physical blocks of a cache handed out, shared, copied and taken back on the device, for all layers that share a
  * block table.  A pool is three DEVICE arrays of the caller's:
- *   refs          int32 [num_blocks]: how many table entries (or other holders) hold the block; 0 or less = free
+ *   refs          int32 [num_blocks]: how many table entries (and other holders, which count themselves in and out) hold the
+ *                 block; 0 or less = free
  *   block_table   int32 [rows][max_blocks_per_seq], as the attention calls read it (row b is sequence b); -1 = no block
- *   context_lens  int32 [rows]; 0 = the row is unused
+ *   context_lens  int32 [rows]; 0 = the row is unused and holds no blocks
  * A new pool has all refs 0, all entries -1, all lengths 0.  Blocks are handed out lowest first, in the order of the call's
  * list, so results depend on the inputs alone.  Calls on one pool (and the attention calls that read its table) are ordered
  * by the stream.
@@ -371,8 +372,9 @@ int coopt_window_prefill(const coopt_cache* cache, const void* q, void* out, con
  *   back, as coopt_window_decode at this length, and any later one, does not read them.  A row named twice is released once.
  * coopt_pages_compact -- the U blocks in use (refs > 0) become the blocks 0 .. U-1: those numbered U and above are copied, in
  *   order, into the free ones below, in every layer.  table_out and refs_out (the pool's own arrays, or others of their size)
- *   get the renumbered table and counts, used_out (DEVICE int32) gets U.  Entries that name a free block, or none of the pool,
- *   become -1 and are reported.  Contents of the blocks from U on are left as they were.
+ *   get the renumbered table and counts, used_out (DEVICE int32) gets U, and new_ids (DEVICE int32 [num_blocks], or NULL) the
+ *   new number of every block, -1 of a free one, for those who hold blocks beside the table.  Entries that name a free block, or
+ *   none of the pool, become -1 and are reported.  Contents of the blocks from U on are left as they were.
  * Errors: INVALID_ARG, UNSUPPORTED (more than 2^20 blocks, 8192 rows or 2^25 blocks a row; 2^31 pairs or blocks times kv heads),
  * WORKSPACE, CUDA.  Every argument is checked before anything is launched.
  */
@@ -394,7 +396,7 @@ int coopt_pages_fork(const coopt_cache* caches, int32_t num_caches, const coopt_
 int coopt_pages_release(const coopt_pages* pages, const int32_t* row_ids, int32_t num_rows, int32_t window, int32_t sinks, void* workspace,
                         size_t workspace_bytes, void* stream);
 int coopt_pages_compact(const coopt_cache* caches, int32_t num_caches, const coopt_pages* pages, int32_t* table_out, int32_t* refs_out, int32_t* used_out,
-                        void* workspace, size_t workspace_bytes, void* stream);
+                        int32_t* new_ids, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Workspace size for a call with these arguments (chunk_size = 0 for coopt_paged_decode).
  * Host arithmetic only (it asks the current device for its SM count once). */

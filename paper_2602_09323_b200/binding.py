@@ -112,7 +112,7 @@ _SIGNATURES = {
     "coopt_pages_release": (ctypes.c_int, [ctypes.POINTER(coopt_pages), ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
                                            ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
     "coopt_pages_compact": (ctypes.c_int, [ctypes.POINTER(coopt_cache), ctypes.c_int32, ctypes.POINTER(coopt_pages), ctypes.c_void_p,
-                                           ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+                                           ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
     "coopt_selftest_bounded_wait": (ctypes.c_int, [ctypes.c_uint64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]),
     "coopt_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "coopt_version": (ctypes.c_int, []),
@@ -431,6 +431,14 @@ else:
         return torch.cuda.current_stream(device).cuda_stream
 
 
+def _int32(x) -> int:
+    """A number that the C interface takes as it is."""
+    x = int(x)
+    if not -0x80000000 <= x <= 0x7FFFFFFF:
+        raise ValueError("numbers have to fit 32 bits")
+    return x
+
+
 def _here(*tensors) -> None:
     """Tensors of the current device, on which the call is enqueued."""
     for t in tensors:
@@ -475,7 +483,7 @@ def window_decode(cache: Cache, q: torch.Tensor, block_table: torch.Tensor, cont
         stride = at[0] if rows > 1 else heads * shape[2]
         k, v, slots = k_new.data_ptr(), v_new.data_ptr(), slot_mapping.data_ptr()
     st = (_lib or load_library()).coopt_window_decode(cache._ref, k, v, stride, slots, q.data_ptr(), out.data_ptr(), block_table.data_ptr(), width[1],
-                                            context_lens.data_ptr(), shape[0], shape[1], window, sinks, sm_scale, workspace.data_ptr(),
+                                            context_lens.data_ptr(), shape[0], shape[1], _int32(window), _int32(sinks), float(sm_scale), workspace.data_ptr(),
                                             workspace.numel(), _stream_of(device))
     if st != 0:
         _check(st, "coopt_window_decode")
@@ -498,7 +506,7 @@ def window_prefill(cache: Cache, q: torch.Tensor, cu_q_lens: torch.Tensor, block
     if not (cu_q_lens.dtype is _I32 and cu_q_lens.is_contiguous() and cu_q_lens.numel() == width[0] + 1 and cu_q_lens.get_device() == device):
         raise ValueError("cu_q_lens: contiguous int32 [B + 1] on the current CUDA device")
     st = (_lib or load_library()).coopt_window_prefill(cache._ref, q.data_ptr(), out.data_ptr(), cu_q_lens.data_ptr(), block_table.data_ptr(), width[1],
-                                             context_lens.data_ptr(), width[0], shape[1], shape[0], window, sinks, sm_scale,
+                                             context_lens.data_ptr(), width[0], shape[1], shape[0], _int32(window), _int32(sinks), float(sm_scale),
                                              workspace.data_ptr(), workspace.numel(), _stream_of(device))
     if st != 0:
         _check(st, "coopt_window_prefill")
@@ -602,15 +610,17 @@ def pages_release(pages: Pages, row_ids: torch.Tensor, workspace: torch.Tensor, 
     device = _device()
     n = _lists(device, row_ids, row_ids)
     _pool_here(device, pages, workspace)
-    st = (_lib or load_library()).coopt_pages_release(pages._ref, row_ids.data_ptr(), n, window, sinks, workspace.data_ptr(), workspace.numel(), _stream_of(device))
+    st = (_lib or load_library()).coopt_pages_release(pages._ref, row_ids.data_ptr(), n, _int32(window), _int32(sinks), workspace.data_ptr(), workspace.numel(), _stream_of(device))
     if st != 0:
         _check(st, "coopt_pages_release")
 
 
 def pages_compact(caches: CacheSet, pages: Pages, workspace: torch.Tensor, table_out: Optional[torch.Tensor] = None,
-                  refs_out: Optional[torch.Tensor] = None, used_out: Optional[torch.Tensor] = None) -> torch.Tensor:
+                  refs_out: Optional[torch.Tensor] = None, used_out: Optional[torch.Tensor] = None,
+                  new_ids: Optional[torch.Tensor] = None) -> torch.Tensor:
     """coopt_pages_compact: the blocks in use become the first ones of the pool; renumbered table and counts into table_out and
-    refs_out (default: in place).  Returns the number of used blocks, an int32 tensor of one element."""
+    refs_out (default: in place), the new number of every block (-1: free) into new_ids.  Returns the number of used blocks, an
+    int32 tensor of one element."""
     device = _device()
     _pool_here(device, pages, workspace, caches)
     table_out = pages.block_table if table_out is None else table_out
@@ -621,8 +631,10 @@ def pages_compact(caches: CacheSet, pages: Pages, workspace: torch.Tensor, table
             and table_out.shape == pages.block_table.shape and refs_out.shape == pages.refs.shape and used_out.numel() == 1
             and table_out.get_device() == refs_out.get_device() == used_out.get_device() == device):
         raise ValueError("table_out, refs_out: like the pool's own; used_out: one int32; on the current CUDA device")
+    if new_ids is not None and not (new_ids.dtype is _I32 and new_ids.is_contiguous() and new_ids.shape == pages.refs.shape and new_ids.get_device() == device):
+        raise ValueError("new_ids: contiguous int32 [num_blocks] on the current CUDA device")
     st = (_lib or load_library()).coopt_pages_compact(caches.array, len(caches.keep), pages._ref, table_out.data_ptr(), refs_out.data_ptr(), used_out.data_ptr(),
-                                            workspace.data_ptr(), workspace.numel(), _stream_of(device))
+                                            new_ids.data_ptr() if new_ids is not None else None, workspace.data_ptr(), workspace.numel(), _stream_of(device))
     if st != 0:
         _check(st, "coopt_pages_compact")
     return used_out

@@ -561,7 +561,7 @@ __global__ void __launch_bounds__(kOneThreads, 1) pages_fork_one_kernel(const __
 }
 
 __global__ void __launch_bounds__(kOneThreads, 1) pages_compact_one_kernel(const __grid_constant__ Copies c, int layers, const Pool pool, int* status, int* counter,
-                                                                           int* table_out, int* refs_out, int* used_out) {
+                                                                           int* table_out, int* refs_out, int* used_out, int* new_ids) {
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ int warp_sums[32], flag;
   wait_previous_kernel();
@@ -612,6 +612,8 @@ __global__ void __launch_bounds__(kOneThreads, 1) pages_compact_one_kernel(const
       if (id >= U) refs_out[id] = 0;                         // (a hole below U gets its mover's count)
     }
   }
+  if (new_ids != nullptr)
+    for (int id = thread; id < pool.blocks; id += threads) new_ids[id] = goes(id);
   const long long entries = static_cast<long long>(pool.rows) * pool.width;
   for (long long e = thread; e < entries; e += threads) {
     int id = pool.table[e];
@@ -923,7 +925,7 @@ int coopt_pages_release(const coopt_pages* pages, const int32_t* row_ids, int32_
 }
 
 int coopt_pages_compact(const coopt_cache* caches, int32_t num_caches, const coopt_pages* pages, int32_t* table_out, int32_t* refs_out, int32_t* used_out,
-                        void* workspace, size_t workspace_bytes, void* stream) {
+                        int32_t* new_ids, void* workspace, size_t workspace_bytes, void* stream) {
   int rc = check_pool(pages, workspace, workspace_bytes);
   if (rc != COOPT_OK) return rc;
   rc = check_caches(caches, num_caches, pages->num_blocks);
@@ -941,11 +943,13 @@ int coopt_pages_compact(const coopt_cache* caches, int32_t num_caches, const coo
     if (!configure_kernel_smem(reinterpret_cast<const void*>(&pages_compact_one_kernel), kMaxOneSmem)) return COOPT_ERR_CUDA;
     const int grid = one_grid(static_cast<long long>(pages->num_blocks / 2) * num_caches * c.heads, entries, di->num_sms);
     return launch_dependent(pages_compact_one_kernel, grid, kOneThreads, smem, st, c, static_cast<int>(num_caches), pool_of(pages), static_cast<int*>(workspace),
-                            one_counter(workspace), static_cast<int*>(table_out), static_cast<int*>(refs_out), static_cast<int*>(used_out))
+                            one_counter(workspace), static_cast<int*>(table_out), static_cast<int*>(refs_out), static_cast<int*>(used_out),
+                            static_cast<int*>(new_ids))
                ? COOPT_OK
                : COOPT_ERR_CUDA;
   }
-  const Plan plan = plan_of(workspace, pages->num_blocks, pages->rows);
+  Plan plan = plan_of(workspace, pages->num_blocks, pages->rows);
+  if (new_ids != nullptr) plan.list = new_ids;
   rc = launch_plan(&pages_compact_plan_kernel, plan_smem(pages, 0), st, pool_of(pages), plan, static_cast<int*>(used_out));
   if (rc != COOPT_OK) return rc;
   c = {};

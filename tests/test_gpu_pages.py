@@ -156,10 +156,14 @@ def test_compaction_of_pools_of_any_size(num_blocks, used):
     p.pages.block_table.copy_(torch.from_numpy(p.ref.table))
     p.pages.refs.copy_(torch.from_numpy(p.ref.refs))
     table_out, refs_out = torch.full_like(p.pages.block_table, 99), torch.full_like(p.pages.refs, 99)
-    count = binding.pages_compact(p.set, p.pages, p.ws, table_out, refs_out)
+    new_ids = torch.full_like(refs_out, 99)
+    old_table, old_refs = p.ref.table.copy(), p.ref.refs.copy()
+    count = binding.pages_compact(p.set, p.pages, p.ws, table_out, refs_out, new_ids=new_ids)
     assert np.array_equal(p.pages.refs.cpu().numpy(), p.ref.refs) and np.array_equal(p.pages.block_table.cpu().numpy(), p.ref.table)
     assert p.ref.compact() == int(count.item()) == used
     assert np.array_equal(table_out.cpu().numpy(), p.ref.table) and np.array_equal(refs_out.cpu().numpy(), p.ref.refs)
+    ids = new_ids.cpu().numpy()
+    assert np.array_equal(ids >= 0, old_refs > 0) and np.array_equal(ids[old_table[old_table >= 0]], p.ref.table[p.ref.table >= 0])
     p.pages.refs.copy_(refs_out), p.pages.block_table.copy_(table_out)
     p.check("apart")
     p.compact()                                           # and once more, in place: nothing moves
@@ -325,6 +329,10 @@ def test_what_the_binding_refuses():
         binding.Pages(p.pages.refs, p.pages.block_table.t(), p.pages.context_lens)
     with pytest.raises(ValueError):
         binding.pages_compact(p.set, p.pages, p.ws, table_out=p.pages.block_table[:2])
+    with pytest.raises(ValueError):
+        binding.pages_compact(p.set, p.pages, p.ws, new_ids=p.pages.refs[:3])
+    with pytest.raises(ValueError):
+        binding.pages_release(p.pages, ints([0]), p.ws, window=2 ** 32 + 5)
     with pytest.raises(ValueError):
         binding.Cache(8, 2, 64, data=torch.zeros(10, dtype=torch.uint8, device="cuda"))
     p.check("nothing happened")

@@ -286,8 +286,46 @@ def test_what_the_binding_refuses():
         binding.window_decode(cache, q, t, n, 9, 1, w.sm_scale, ws, k_new=q[:, :2])
     with pytest.raises(ValueError):
         binding.window_prefill(cache, q, torch.arange(3, dtype=torch.int32).cuda(), t, n, 9, 1, w.sm_scale, ws)
+    with pytest.raises(ValueError):
+        binding.window_decode(cache, q, t, n, 2 ** 32 + 9, 1, w.sm_scale, ws)
     for window, sinks in ((0, 1), (-1, 0), (5, -1)):
         with pytest.raises(binding.CooptError):
             binding.window_decode(cache, q, t, n, window, sinks, w.sm_scale, ws)
     with pytest.raises(binding.CooptError):
         binding.window_decode(cache, q, t, n, 9, 1, w.sm_scale, ws[:1000])
+
+
+def test_two_streams_at_once():
+    """Calls that overlap on the device, each with a workspace of its own."""
+    lens = [2500, 4, 900, 1300, 77, 3000]
+    w, cache, kv, table = make(lens, [1] * 6, 16, 4, 64, "e4m3", 1000, 4, seed=43)
+    want = decode(w, cache, table, lens, 1000, 4)
+    q, t, n = w.q.cuda(), table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda()
+    cu = torch.arange(7, dtype=torch.int32).cuda()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    spaces = [binding.new_workspace(6, 16, 4, 64, table.shape[1]) for _ in streams]
+    outs = [[torch.zeros_like(q) for _ in range(20)] for _ in streams]
+    torch.cuda.synchronize()
+    for turn in range(20):
+        for k, (stream, ws) in enumerate(zip(streams, spaces)):
+            with torch.cuda.stream(stream):
+                if k < 2:
+                    binding.window_decode(cache, q, t, n, 1000, 4, w.sm_scale, ws, out=outs[k][turn])
+                else:
+                    binding.window_prefill(cache, q, cu, t, n, 1000, 4, w.sm_scale, ws, out=outs[k][turn])
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for k in range(2) for o in outs[k])
+    assert all(torch.equal(o, outs[2][0]) for o in outs[2])
+    ref, spread = attention.window_attention(w.q.float().numpy(), kv, w.block_table.numpy(), lens, 1000, 4)
+    check(outs[2][0], ref, spread, "e4m3", prefill=True, vmax=6.0)
+
+
+@pytest.mark.parametrize("batch,hkv,window", [(1, 1, 3000), (3, 8, 200), (19, 8, 700), (33, 8, 900), (52, 8, 500), (60, 8, 400), (150, 1, 1100), (301, 1, 350)])
+def test_every_way_of_sharing_out_the_work(batch, hkv, window):
+    """From a cluster to a unit over one, two and three CTAs on an SM to the line, with contexts of all lengths beside each other."""
+    lens = [(b * 7919) % (2 * window) for b in range(batch)]
+    lens[0] = 2 * window + 1
+    for fmt, dim in (("e4m3", 128), ("bf16", 64)):
+        w, cache, kv, table = make(lens, [1] * batch, 2 * hkv, hkv, dim, fmt, window, 9, seed=47 + batch)
+        ref, spread = attention.window_attention(w.q.float().numpy(), kv, w.block_table.numpy(), lens, window, 9)
+        check(decode(w, cache, table, lens, window, 9), ref, spread, fmt, what=f"{fmt} {batch}")

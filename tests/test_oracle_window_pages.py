@@ -114,7 +114,7 @@ def test_refusals_on_the_host():
         "reserve": lambda p, ws=0x100, size=n, a=0x100, b=0x100, k=1: lib.coopt_pages_reserve(p, a, b, k, ws, size, None),
         "fork": lambda p, ws=0x100, size=n, a=0x100, b=0x100, k=1: lib.coopt_pages_fork(one, 1, p, a, b, k, ws, size, None),
         "release": lambda p, ws=0x100, size=n, a=0x100, b=0x100, k=1: lib.coopt_pages_release(p, a, k, 0, 0, ws, size, None),
-        "compact": lambda p, ws=0x100, size=n, a=0x100, b=0x100, k=1: lib.coopt_pages_compact(one, 1, p, a, b, 0x100, ws, size, None),
+        "compact": lambda p, ws=0x100, size=n, a=0x100, b=0x100, k=1: lib.coopt_pages_compact(one, 1, p, a, b, 0x100, None, ws, size, None),
     }
     for name, call in calls.items():
         ref = lambda **k: ctypes.byref(pool(**k))     # noqa: E731
