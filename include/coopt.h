@@ -322,8 +322,10 @@ int coopt_decode_step_host(const coopt_cache* cache, const void* step_inputs_hos
  *
  * coopt_window_decode -- one query token per sequence, at position context_lens[b] - 1; the arguments of coopt_paged_decode.
  *   k_new, v_new, slot_mapping  the step's new tokens, written first, as for coopt_decode_step_planned (the same precondition:
- *                               the new token of sequence b is its last position; FP8 caches take them in the same launch, a
- *                               bf16 cache by coopt_kv_write's rule in a launch of its own); all three NULL = none
+ *                               the new token of sequence b is its last position).  FP8 caches take them in the same launch, by
+ *                               coopt_kv_write's rule but for the rounding of the scale: amax times the fp32 reciprocal of 448
+ *                               (57344), at most one unit in the last place from amax / 448.  A bf16 cache takes them in a
+ *                               launch of its own.  All three NULL = none
  *   context_lens                counting the new token; 0 gives an all-zero output row
  * coopt_window_prefill -- runs of query tokens; the arguments of coopt_paged_chunked without chunks, always causal.
  *   cu_q_lens                   runs may have any length, 0 and 1 included; total_q = cu_q_lens[batch] sizes the launch, and rows

@@ -53,8 +53,11 @@ def _quantise(x: np.ndarray, scale: np.float32, fmt=e4m3) -> np.ndarray:
 
 
 def kv_write(codes: np.ndarray, scales: np.ndarray, k: np.ndarray, v: np.ndarray,
-             slot_mapping: np.ndarray, heads=None, fmt=e4m3) -> None:
+             slot_mapping: np.ndarray, heads=None, fmt=e4m3, reciprocal: bool = False) -> None:
     """Apply one write call in place.
+
+    ``reciprocal``: the scale of a group is amax times the rounded reciprocal of fmt.MAX (one rounding more) instead of
+    their quotient, as the append of a windowed decode step has it.
 
     ``fmt`` is the 8-bit format of the codes: ``e4m3`` (the reading the build takes), or ``e5m2``
     as an ablation of the format the paper leaves open; the scale is amax / fmt.MAX either way.
@@ -78,7 +81,7 @@ def kv_write(codes: np.ndarray, scales: np.ndarray, k: np.ndarray, v: np.ndarray
                 x = kv[w][tok, h, :]                              # [n, D]
                 amax = _F32(np.max(np.abs(x)))
                 s_old = _F32(0.0) if fresh else _F32(scales[blk, h, w])
-                s_new = max(s_old, _F32(amax / _F32(fmt.MAX)))
+                s_new = max(s_old, _F32(amax * (_F32(1.0) / _F32(fmt.MAX))) if reciprocal else _F32(amax / _F32(fmt.MAX)))
                 if fresh:
                     codes[blk, h, w, others, :] = 0
                 elif s_new > s_old and s_old > 0:

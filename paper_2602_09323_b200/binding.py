@@ -473,14 +473,14 @@ def window_decode(cache: Cache, q: torch.Tensor, block_table: torch.Tensor, cont
     stride, k, v, slots = 0, None, None, None
     if k_new is not None or v_new is not None or slot_mapping is not None:
         _need(k_new is not None and v_new is not None and slot_mapping is not None, "k_new, v_new and slot_mapping go together")
-        rows, heads, at = shape[0], cache.num_kv_heads, k_new.stride()
-        if not (k_new.shape == v_new.shape == (rows, heads, shape[2]) and k_new.dtype is _BF16 and v_new.dtype is _BF16 and at == v_new.stride()
-                and at[2] == 1 and (at[1] == shape[2] or heads == 1)):
-            raise ValueError("k_new, v_new: bf16 [B, Hkv, D] of the same strides, heads and dims dense")
-        if not (slot_mapping.dtype is _I64 and slot_mapping.is_contiguous() and slot_mapping.numel() == rows):
-            raise ValueError("slot_mapping: contiguous int64 [B]")
-        _here(k_new, v_new, slot_mapping)
-        stride = at[0] if rows > 1 else heads * shape[2]
+        rows, heads, dim = shape[0], cache.num_kv_heads, shape[2]
+        at = k_new.stride()
+        if not (k_new.shape == v_new.shape == (rows, heads, dim) and at == v_new.stride() and at[2] == 1 and (at[1] == dim or heads == 1)
+                and k_new.dtype is v_new.dtype is _BF16 and slot_mapping.dtype is _I64 and slot_mapping.is_contiguous()
+                and slot_mapping.numel() == rows and k_new.get_device() == v_new.get_device() == slot_mapping.get_device() == device):
+            raise ValueError("k_new, v_new: bf16 [B, Hkv, D] of the same strides, heads and dims dense; slot_mapping: contiguous int64 [B]; "
+                             "on the current CUDA device")
+        stride = at[0] if rows > 1 else heads * dim
         k, v, slots = k_new.data_ptr(), v_new.data_ptr(), slot_mapping.data_ptr()
     st = (_lib or load_library()).coopt_window_decode(cache._ref, k, v, stride, slots, q.data_ptr(), out.data_ptr(), block_table.data_ptr(), width[1],
                                             context_lens.data_ptr(), shape[0], shape[1], _int32(window), _int32(sinks), float(sm_scale), workspace.data_ptr(),

@@ -1,5 +1,6 @@
 // Host side of the C ABI: argument checks, workspace arithmetic, dispatch to the launchers.
 #include <algorithm>
+#include <atomic>
 #include <mutex>
 #include <utility>
 #include <vector>
@@ -16,18 +17,19 @@ int launch_paged_prefill(const coopt_cache* c, const void* q, void* out, const i
                          float sm_scale, void* workspace, int num_sms, cudaStream_t stream);
 const DeviceInfo* device_info() {
   static DeviceInfo info[64];
-  static bool known[64] = {};
+  static std::atomic<bool> known[64];
   static std::mutex mu;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
+  if (known[dev].load(std::memory_order_acquire)) return &info[dev];      // (asked several times a call)
   std::lock_guard<std::mutex> lock(mu);
-  if (!known[dev]) {
+  if (!known[dev].load(std::memory_order_relaxed)) {
     int sms = 0, smem = 0;
     if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return nullptr;
     if (cudaDeviceGetAttribute(&smem, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev) != cudaSuccess) return nullptr;
     info[dev].num_sms = sms;
     info[dev].max_smem_optin = smem;
-    known[dev] = true;
+    known[dev].store(true, std::memory_order_release);
   }
   return &info[dev];
 }

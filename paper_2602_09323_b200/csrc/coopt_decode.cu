@@ -197,7 +197,10 @@ template <bool kE5m2> __device__ __forceinline__ uint32_t codes_hi(uint32_t w) {
 // Algorithm 1 phase 1 for one token, on the granule as it sits in shared memory (K part, V part, header), which is then
 // written back: the write kernels' rule (write_part), with the same value for every number that is stored.
 // k, v: this lane's D / 32 consecutive values of the token's rows, as packed pairs.
-template <int D, bool kE5m2>
+// kReciprocal (windowed calls): the scale of the token's largest magnitude is that times the rounded reciprocal of the format's
+// largest value, and not the quotient, from which it differs by one unit in the last place at most.  The codes follow from
+// the scale by the same rule (a value that then lies beyond the largest code by a rounding takes that code).
+template <int D, bool kE5m2, bool kReciprocal>
 __device__ __noinline__ void append_token(uint8_t* st, uint8_t* gran, const uint2 k, const uint2 v, int off, int lane) {
   constexpr int kPart = kBlockSize * D, kPerLane = D / 32;
   float* hdr = reinterpret_cast<float*>(st + header_offset(D));
@@ -210,7 +213,8 @@ __device__ __noinline__ void append_token(uint8_t* st, uint8_t* gran, const uint
     if (kPerLane == 4) amax2 = __vmaxu2(amax2, raw[which][1] & 0x7FFF7FFFu);
     const uint32_t am = __reduce_max_sync(0xffffffffu, max(amax2 << 16, amax2 & 0xFFFF0000u));   // non-negative floats order like their bits
     s_old[which] = fresh ? 0.0f : hdr[which];
-    s_new[which] = fmaxf(s_old[which], __fdiv_rn(__uint_as_float(am), kE5m2 ? kE5m2Max : kE4m3Max));
+    constexpr float kMax = kE5m2 ? kE5m2Max : kE4m3Max;
+    s_new[which] = fmaxf(s_old[which], kReciprocal ? __fmul_rn(__uint_as_float(am), 1.0f / kMax) : __fdiv_rn(__uint_as_float(am), kMax));
   }
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
@@ -859,7 +863,7 @@ paged_decode_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
             if (slot != static_cast<long long>(id) * kBlockSize + off) {     // not the sequence's last position
               if (lane == 0) atomicCAS(p.status, 0, COOPT_ERR_INVALID_ARG);
             } else if (id >= 0 && id < p.num_blocks) {
-              append_token<D, C::kE5m2>(st, layer(y).cache + (static_cast<size_t>(id) * Hkv + work_walk->g) * C::kGran, k_row, v_row, off, lane);
+              append_token<D, C::kE5m2, kWindow>(st, layer(y).cache + (static_cast<size_t>(id) * Hkv + work_walk->g) * C::kGran, k_row, v_row, off, lane);
             }
             __syncwarp();
           }

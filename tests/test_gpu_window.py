@@ -12,7 +12,7 @@ import numpy as np
 import pytest
 import torch
 
-from oracle import attention, e4m3, e5m2
+from oracle import attention, e4m3, e5m2, kv_cache
 from paper_2602_09323_b200 import binding, workloads
 from tests import helpers
 
@@ -156,18 +156,30 @@ def test_a_window_over_everything_is_the_call_without_one(fmt):
 
 @pytest.mark.parametrize("fmt,dim", [("e4m3", 128), ("e5m2", 64), ("bf16", 64)])
 def test_new_tokens_are_written_and_seen(fmt, dim):
-    """Step after step over a sliding window: the cache's bytes are kv_write's, the output is that of the two calls, and what
-    has left the window is taken out of the table as it goes.  K and V are slices of one wider projection."""
+    """Step after step over a sliding window: the cache's bytes are those of the write rule, the output is that of the call
+    over the written cache, and what has left the window is taken out of the table as it goes.  K and V are slices of one wider
+    projection."""
     lens0, window, sinks, steps, hkv, hq = [14, 30, 100, 0, 257], 33, 5, 20, 2, 6
     B = len(lens0)
     w = workloads.make_workload("steps", [L + steps for L in lens0], hq, hkv, dim, seed=19)
     width = w.block_table.shape[1]
-    one, two = (binding.Cache(w.num_blocks, hkv, dim, FMT[fmt]) for _ in range(2))
+    cache = binding.Cache(w.num_blocks, hkv, dim, FMT[fmt])
+    kind = {"e4m3": e4m3, "e5m2": e5m2}.get(fmt)
+    codes, scales = kv_cache.new_cache(w.num_blocks, hkv, dim)
+    values = kv_cache.new_cache_bf16(w.num_blocks, hkv, dim)
+
+    def oracle_write(rows, slots, **more):
+        k, v, slots = w.k[rows].float().numpy(), w.v[rows].float().numpy(), slots.numpy()
+        if fmt == "bf16":
+            kv_cache.kv_write_bf16(values, k, v, slots)
+        else:
+            kv_cache.kv_write(codes, scales, k, v, slots, fmt=kind, **more)
+
     for b, L in enumerate(lens0):
         if L:
             rows = slice(w.kv_offsets[b], w.kv_offsets[b] + L)
-            for c in (one, two):
-                binding.kv_write(c, w.k[rows].cuda(), w.v[rows].cuda(), w.slot_mapping[rows].cuda())
+            binding.kv_write(cache, w.k[rows].cuda(), w.v[rows].cuda(), w.slot_mapping[rows].cuda())
+            oracle_write(rows, w.slot_mapping[rows])
     ws, ws2 = (binding.new_workspace(B, hq, hkv, dim, width) for _ in range(2))
     table = w.block_table.cuda()
     for s in range(steps):
@@ -183,14 +195,17 @@ def test_new_tokens_are_written_and_seen(fmt, dim):
         k, v, slots = wide[:, hkv:2 * hkv], wide[:, 2 * hkv:], w.slot_mapping[rows].clone()
         if s == 7:
             slots[2] = -1                                   # a token that is not stored
+        oracle_write(rows, slots, **({} if fmt == "bf16" else {"reciprocal": True}))
         slots, q = slots.cuda(), torch.randn(B, hq, dim).to(torch.bfloat16).cuda()
         lens_t = torch.tensor(lens, dtype=torch.int32).cuda()
-        out = binding.window_decode(one, q, table, lens_t, window, sinks, w.sm_scale, ws, k, v, slots)
-        binding.kv_write(two, k.contiguous(), v.contiguous(), slots)
-        want = binding.window_decode(two, q, table, lens_t, window, sinks, w.sm_scale, ws2)
+        out = binding.window_decode(cache, q, table, lens_t, window, sinks, w.sm_scale, ws, k, v, slots)
+        want = binding.window_decode(cache, q, table, lens_t, window, sinks, w.sm_scale, ws2)
         torch.cuda.synchronize()
         assert binding.workspace_status(ws) == 0 and binding.workspace_status(ws2) == 0
-        assert torch.equal(one.data, two.data), f"step {s}"
+        if fmt == "bf16":
+            assert np.array_equal(helpers.cache_to_logical(cache), values), f"step {s}"
+        else:
+            helpers.check_cache_bit_exact(cache, codes, scales, what=f"step {s}")
         assert torch.equal(out, want), f"step {s}"
 
 

@@ -135,3 +135,21 @@ def test_refusals_on_the_host():
     assert copy(two(dim=96), 2) == -2 and copy(two(data=0), 2) == -1 and copy(one, 1, m=2 ** 30) == -2
     assert lib.coopt_pages_fork((binding.coopt_cache * 1)(cache(blocks=9)), 1, p, 0x100, 0x100, 1, 0x100, n, None) == -1
     assert binding.status_string(-6).startswith("too few")
+
+
+def test_the_reciprocal_rule_is_within_an_ulp_of_the_quotient():
+    from oracle import e4m3, e5m2, kv_cache
+    rng = np.random.default_rng(11)
+    differ = 0
+    for fmt in (e4m3, e5m2):
+        for trial in range(200):
+            k, v = (rng.standard_normal((1, 1, 8)).astype(np.float32) * np.float32(10.0 ** rng.integers(-3, 4)) for _ in range(2))
+            one, two = kv_cache.new_cache(1, 1, 8), kv_cache.new_cache(1, 1, 8)
+            kv_cache.kv_write(*one, k, v, np.array([0]), fmt=fmt)
+            kv_cache.kv_write(*two, k, v, np.array([0]), fmt=fmt, reciprocal=True)
+            a, b = one[1].view(np.int32).astype(np.int64), two[1].view(np.int32).astype(np.int64)
+            assert np.all(np.abs(a - b) <= 1)
+            differ += int(np.sum(a != b))
+            # the largest value still takes the largest code
+            assert np.isclose(np.abs(fmt.decode(two[0])).max(), fmt.MAX)
+    assert differ > 0
