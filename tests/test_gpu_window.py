@@ -344,3 +344,17 @@ def test_every_way_of_sharing_out_the_work(batch, hkv, window):
         w, cache, kv, table = make(lens, [1] * batch, 2 * hkv, hkv, dim, fmt, window, 9, seed=47 + batch)
         ref, spread = attention.window_attention(w.q.float().numpy(), kv, w.block_table.numpy(), lens, window, 9)
         check(decode(w, cache, table, lens, window, 9), ref, spread, fmt, what=f"{fmt} {batch}")
+
+
+@pytest.mark.parametrize("group,hkv,batch,most,context,window,sinks", [(1, 8, 12, 300, 3000, 40, 4), (5, 8, 9, 130, 2000, 300, 0), (8, 8, 40, 40, 500, 100, 20),
+                                                                     (4, 4, 3, 1500, 1500, 200, 3), (2, 8, 20, 64, 4000, 1000, 1)])
+def test_prefill_of_several_rounds(group, hkv, batch, most, context, window, sinks):
+    """More pieces of work than the device takes at a time: which goes where, and in what order, is worked out on the device."""
+    rng = np.random.default_rng(batch)
+    q_lens = [int(x) for x in rng.integers(0, most + 1, batch)]
+    q_lens[0], q_lens[-1] = most, 128 // group                # a whole tile
+    lens = [n + int(x) for n, x in zip(q_lens, rng.integers(0, max(1, context - most), batch))]
+    w, cache, kv, table = make(lens, q_lens, group * hkv, hkv, 64, "e4m3", window, sinks, seed=61 + batch)
+    out = prefill(w, cache, table, window, sinks, extra_rows=2)
+    ref, spread = attention.window_attention(w.q.float().numpy(), kv, w.block_table.numpy(), lens, window, sinks, w.cu_q_lens.numpy())
+    check(out, ref, spread, "e4m3", prefill=True, vmax=6.0)
