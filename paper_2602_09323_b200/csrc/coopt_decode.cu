@@ -259,8 +259,9 @@ struct Acc {
 };
 __device__ __forceinline__ void acc_clear(Acc& a) { a.M = -INFINITY; a.den = 0.0f; a.num = make_float4(0.0f, 0.0f, 0.0f, 0.0f); }
 // Up to 32 more pieces into the accumulator.  Lane k brings piece k's maximum and sum; `rows(k)` is where the piece's o
-// (normalised by its sum) lies for this lane.
-template <bool kGlobal, class Rows>
+// (normalised by its sum) lies for this lane.  kNan: a piece whose sum is NaN (a key that is seen was) makes the result NaN; else
+// it is left out.
+template <bool kGlobal, bool kNan, class Rows>
 __device__ __forceinline__ void acc_merge(Acc& a, int n, float m, float l, bool on, Rows rows) {
   constexpr int kUnroll = 4;
   float4 o[kUnroll];
@@ -272,7 +273,7 @@ __device__ __forceinline__ void acc_merge(Acc& a, int n, float m, float l, bool 
     }
   };
   fetch(0);                              // (on their way while the weights are worked out)
-  const bool some = l > 0.0f;
+  const bool some = kNan ? !(l <= 0.0f) : l > 0.0f;
   const float top = fmaxf(a.M, ordered_to_f32(__reduce_max_sync(0xffffffffu, f32_to_ordered(some ? m : -INFINITY))));
   const float wgt = some ? l * ex2(m - top) : 0.0f;
   const float keep = a.den > 0.0f ? ex2(a.M - top) : 0.0f;
@@ -284,7 +285,7 @@ __device__ __forceinline__ void acc_merge(Acc& a, int n, float m, float l, bool 
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k) {
       const float w = k0 + k < n ? __shfl_sync(0xffffffffu, wgt, k0 + k) : 0.0f;
-      if (w > 0.0f) { a.num.x += w * o[k].x; a.num.y += w * o[k].y; a.num.z += w * o[k].z; a.num.w += w * o[k].w; }
+      if (kNan ? !(w <= 0.0f) : w > 0.0f) { a.num.x += w * o[k].x; a.num.y += w * o[k].y; a.num.z += w * o[k].z; a.num.w += w * o[k].w; }
     }
     k0 += kUnroll;
     if (k0 >= n) break;
@@ -296,7 +297,7 @@ __device__ __forceinline__ void acc_merge(Acc& a, int n, float m, float l, bool 
 // Pieces of the warps of a CTA lie in shared memory.  A head of a piece that other shares hold the rest of goes to the
 // workspace, and is counted; who counts the last one takes them all and finishes the unit.  The first piece of a unit lies
 // in the odd slot of its share, the others in the even ones.
-template <int D, int FMT, int L>
+template <int D, int FMT, int L, bool kWindow>
 struct Merge {
   using C = Cfg<D, FMT>;
   const DecodeParams& p;
@@ -340,7 +341,7 @@ struct Merge {
       const int n = min(32, pieces - c0);
       auto slot = [&](int c) { return slot_of(region, cta_f + c, c == 0, h); };
       const float m = lane < n ? __ldcg(p.run_m + slot(c0 + lane)) : 0.0f, l = lane < n ? __ldcg(p.run_l + slot(c0 + lane)) : 0.0f;
-      acc_merge<true>(a, n, m, l, on(), [&](int k) { return p.run_o + slot(c0 + k) * D + lane * 4; });
+      acc_merge<true, kWindow>(a, n, m, l, on(), [&](int k) { return p.run_o + slot(c0 + k) * D + lane * 4; });
     }
   }
   __device__ __forceinline__ void store_out(const Acc& a, int b, int g, int h) const {
@@ -387,7 +388,7 @@ struct Merge {
       const int n = last - from + 1;
       Acc a;
       acc_clear(a);
-      acc_merge<false>(a, n, lane < n ? piece(lane)[D] : 0.0f, lane < n ? piece(lane)[D + 1] : 0.0f, on(), [&](int k) { return piece(k) + lane * 4; });
+      acc_merge<false, kWindow>(a, n, lane < n ? piece(lane)[D] : 0.0f, lane < n ? piece(lane)[D + 1] : 0.0f, on(), [&](int k) { return piece(k) + lane * 4; });
       if (kind && closed) {
         finish(a, b, g, h, u);
       } else {
@@ -1077,14 +1078,14 @@ paged_decode_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
   if constexpr (kFew) {
     __syncthreads();
     // A head to a warp: the pieces of this CTA's warps, then, over distributed shared memory, of the cluster's CTAs.
-    Merge<D, FMT, L> merge{p, table, ln, smem, recs, 0u, piece0_off, piece1_off, warp, lane, 0};
+    Merge<D, FMT, L, kWindow> merge{p, table, ln, smem, recs, 0u, piece0_off, piece1_off, warp, lane, 0};
     auto piece = [&](int k, int h) { return reinterpret_cast<float*>(smem + k * C::kWarpBytes + piece0_off) + h * C::kPieceStride; };
     const int heads = lens[few_b] > 0 ? G : 0;
 #pragma unroll 1
     for (int h = warp; h < heads; h += C::kWarps) {
       Acc a;
       acc_clear(a);
-      acc_merge<false>(a, C::kWarps, lane < C::kWarps ? piece(lane, h)[D] : 0.0f, lane < C::kWarps ? piece(lane, h)[D + 1] : 0.0f, merge.on(),
+      acc_merge<false, kWindow>(a, C::kWarps, lane < C::kWarps ? piece(lane, h)[D] : 0.0f, lane < C::kWarps ? piece(lane, h)[D + 1] : 0.0f, merge.on(),
                        [&](int k) { return piece(k, h) + lane * 4; });
       if (p.splits == 1) {
         merge.store_out(a, few_b, few_g, h);
@@ -1112,11 +1113,11 @@ paged_decode_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
             ml[s] = ld_cluster_f2(at + D * 4, s);
             o[s] = ld_cluster_f4(at + (merge.on() ? lane : 0) * 16, s);
           }
-          if (ml[s].y > 0.0f) a.M = fmaxf(a.M, ml[s].x);
+          if (!(ml[s].y <= 0.0f)) a.M = fmaxf(a.M, ml[s].x);
         }
 #pragma unroll
         for (int s = 0; s < kMaxSplits; ++s) {
-          if (ml[s].y > 0.0f) {
+          if (!(ml[s].y <= 0.0f)) {      // (NaN: as in acc_merge)
             const float f = ex2(ml[s].x - a.M);
             a.den += ml[s].y * f;
             a.num.x += o[s].x * f; a.num.y += o[s].y * f; a.num.z += o[s].z * f; a.num.w += o[s].w * f;
@@ -1150,7 +1151,7 @@ paged_decode_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
   }
   COOPT_TRACE_CYCLES(p.trace, kTrStreamed, tid == 0);
 
-  Merge<D, FMT, L> merge{p, table, ln, smem, recs, cut[1], piece0_off, piece1_off, warp, lane, y};
+  Merge<D, FMT, L, kWindow> merge{p, table, ln, smem, recs, cut[1], piece0_off, piece1_off, warp, lane, y};
   merge.local(v_share);
   if (L > 1 || p.chunk_blocks == 0) {
     __syncwarp();
@@ -1198,7 +1199,7 @@ paged_decode_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
           m = cut(i) ? __ldcg(p.run_m + slot(i)) : __ldcg(p.part_m + rows + i) * kLog2e;
           l = cut(i) ? __ldcg(p.run_l + slot(i)) * kUnshift : __ldcg(p.part_l + rows + i);
         }
-        acc_merge<true>(a, n, m, l, merge.on(), [&](int k) { return (cut(c0 + k) ? p.run_o + slot(c0 + k) * D : p.part_o + (rows + c0 + k) * D) + lane * 4; });
+        acc_merge<true, kWindow>(a, n, m, l, merge.on(), [&](int k) { return (cut(c0 + k) ? p.run_o + slot(c0 + k) * D : p.part_o + (rows + c0 + k) * D) + lane * 4; });
       }
       if (run_begins && run_ends) {
         merge.store_out(a, b, g, h);

@@ -514,7 +514,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
     ok = __all_sync(0xffffffffu, ok);
     if (ok) {
       tc_fence_after();
-      const float k = l_row > 0.0f ? v_ref / l_row : 0.0f;
+      const float k = (kWindow ? !(l_row <= 0.0f) : l_row > 0.0f) ? v_ref / l_row : 0.0f;      // (kWindow: a NaN sum makes the row NaN)
       // The rows go through shared memory, where the tile's query operand was (its products are done): 16 bytes of a row at
       // (chunk ^ row).
       if constexpr (kSplit) {
@@ -862,12 +862,12 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
           }
 #pragma unroll
           for (int s = 0; s < kMaxSplits; ++s)
-            if (ml[s].y > 0.0f) top = fmaxf(top, ml[s].x);
+            if (!(ml[s].y <= 0.0f)) top = fmaxf(top, ml[s].x);
           float den = 0.0f;
           float4 num = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
           for (int s = 0; s < kMaxSplits; ++s) {
-            if (ml[s].y > 0.0f) {
+            if (!(ml[s].y <= 0.0f)) {    // (a NaN sum, of a key that is seen, is not left out)
               const float w = ml[s].y * ex2(ml[s].x - top);
               den += w;
               num.x += w * o[s].x; num.y += w * o[s].y; num.z += w * o[s].z; num.w += w * o[s].w;

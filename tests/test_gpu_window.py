@@ -358,3 +358,35 @@ def test_prefill_of_several_rounds(group, hkv, batch, most, context, window, sin
     out = prefill(w, cache, table, window, sinks, extra_rows=2)
     ref, spread = attention.window_attention(w.q.float().numpy(), kv, w.block_table.numpy(), lens, window, sinks, w.cu_q_lens.numpy())
     check(out, ref, spread, "e4m3", prefill=True, vmax=6.0)
+
+
+@pytest.mark.parametrize("lens,q_lens", [([403, 64], [4, 3]), ([403, 64], [40, 30]), ([3000, 64], [200, 3]), ([700, 90] * 80, [30, 9] * 80)])
+def test_a_key_that_is_nan_reaches_those_who_see_it_and_no_one_else(lens, q_lens):
+    """The last token's key of kv head 0, in each of the ways that a run is served."""
+    w, cache, kv, table = make(lens, q_lens, 10, 2, 128, "e4m3", 200, 3, seed=73)
+    before = prefill(w, cache, table, 200, 3)
+    spoil_last_key(w, cache, table, lens)
+    after = prefill(w, cache, table, 200, 3)
+    last = torch.zeros(len(before), dtype=torch.bool)
+    last[w.cu_q_lens[1:].long() - 1] = True
+    assert torch.isnan(after[last][:, :5].float()).all()
+    assert torch.equal(before[~last], after[~last]) and torch.equal(before[:, 5:], after[:, 5:])
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "bf16"])
+@pytest.mark.parametrize("lens", [[17], [2000], [350, 900] * 10, [40, 900] * 25, [350, 900, 3] * 40])
+def test_a_token_whose_key_is_nan_makes_the_output_nan(lens, fmt):
+    w, cache, kv, table = make(lens, [1] * len(lens), 10, 2, 128, fmt, 800, 3, seed=79)
+    before = decode(w, cache, table, lens, 800, 3)
+    spoil_last_key(w, cache, table, lens)
+    after = decode(w, cache, table, lens, 800, 3)
+    assert torch.isnan(after[:, :5].float()).all() and torch.equal(before[:, 5:], after[:, 5:])
+
+
+def spoil_last_key(w, cache, table, lens):
+    raw = cache.data.view(w.num_blocks, w.num_kv_heads, cache.granule_bytes)
+    idx = torch.from_numpy(helpers.granule_index_map(cache))
+    for b, L in enumerate(lens):
+        at = idx[0, (L - 1) % 16].cuda()
+        for byte in range(1 if cache.dtype != FMT["bf16"] else 2):
+            raw[int(table[b, (L - 1) // 16]), 0, at + byte] = 0x7F if cache.dtype != FMT["bf16"] or byte == 1 else 0xC0
