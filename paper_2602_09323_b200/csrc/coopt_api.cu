@@ -14,7 +14,7 @@ int launch_kv_write(const coopt_cache* c, const void* k, const void* v, int64_t 
 int launch_paged_prefill(const coopt_cache* c, const void* q, void* out, const int32_t* cu_q_lens,
                          const int32_t* block_table, int32_t max_blocks_per_seq, const int32_t* context_lens,
                          int32_t batch, int32_t num_q_heads, int32_t total_q, int32_t causal, int32_t window, int32_t sinks,
-                         float sm_scale, void* workspace, int num_sms, cudaStream_t stream);
+                         float sm_scale, void* workspace, int num_sms, cudaStream_t stream, DecodeCall* rows);
 const DeviceInfo* device_info() {
   static DeviceInfo info[64];
   static std::atomic<bool> known[64];
@@ -497,7 +497,7 @@ int coopt_paged_chunked(const coopt_cache* cache, const void* q, void* out, cons
     return launch_decode(a, static_cast<cudaStream_t>(stream));
   }
   return launch_paged_prefill(cache, q, out, cu_q_lens, block_table, max_blocks_per_seq, context_lens, batch,
-                              num_q_heads, total_q, causal, 0, 0, sm_scale, workspace, num_sms(), static_cast<cudaStream_t>(stream));
+                              num_q_heads, total_q, causal, 0, 0, sm_scale, workspace, num_sms(), static_cast<cudaStream_t>(stream), nullptr);
 }
 
 // Windows and sinks beyond any context mean the same as the longest one; sums of them and positions stay inside 32 bits.
@@ -558,8 +558,17 @@ int coopt_window_prefill(const coopt_cache* cache, const void* q, void* out, con
   if (!workspace || workspace_bytes < workspace_control_bytes()) return COOPT_ERR_WORKSPACE;
   window = within_context(window);
   sinks = within_context(sinks);
+  const coopt_layer_io io = {cache, nullptr, nullptr, nullptr, q, out};
+  DecodeCall rows = attention_call(&io, 1, max_blocks_per_seq, total_q, num_q_heads, 0, sm_scale, workspace);   // a row for every token
+  rows.block_table = block_table;
+  rows.context_lens = context_lens;
+  rows.cu_q_lens = cu_q_lens;
+  rows.sequences = batch;
+  rows.window = window;
+  rows.sinks = sinks;
+  const bool few = total_q <= decode_max_batch() && batch <= decode_max_batch();
   return launch_paged_prefill(cache, q, out, cu_q_lens, block_table, max_blocks_per_seq, context_lens, batch, num_q_heads, total_q, 1,
-                              window, sinks, sm_scale, workspace, num_sms(), static_cast<cudaStream_t>(stream));
+                              window, sinks, sm_scale, workspace, num_sms(), static_cast<cudaStream_t>(stream), few ? &rows : nullptr);
 }
 
 namespace {

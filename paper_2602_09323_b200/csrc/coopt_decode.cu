@@ -31,6 +31,7 @@
 #include <float.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "coopt_decode.cuh"
 #include "coopt_trace.cuh"
@@ -421,7 +422,8 @@ struct Merge {
 // one streams while another starts or joins.  (40 heads over 8, head_dim 128, E4M3, us as a line / so: one sequence, window 30
 // 11.3 / 5.6, 1024 12.3 / 7.2, 4096 14.2 / 9.7; 18 sequences, window 250 10.0 / 7.6, 2048 22.9 / 18.0; 32 sequences, two CTAs an
 // SM, window 250 16.0 / 9.2, 2048 32.9 / 27.7; 50, three, window 250 18.0 / 10.4.)
-template <int D, int FMT, int L, bool kWindow, int kFewPerSm>
+// kRuns: the rows are query tokens of runs (see kRunNs; a build of its own, as the rest lost 1.5 % by the choice).
+template <int D, int FMT, int L, bool kWindow, int kFewPerSm, bool kRuns>
 __global__ void __launch_bounds__(Cfg<D, FMT, kFewPerSm ? kFewPerSm : kCtasPerSm>::kThreads, kFewPerSm ? kFewPerSm : kCtasPerSm)
 paged_decode_kernel(const __grid_constant__ DecodeParams p, const __grid_constant__ LayerTable<L> table) {
   constexpr bool kFew = kFewPerSm > 0;
@@ -465,19 +467,31 @@ paged_decode_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
   if (p.order == kDependent) wait_previous_kernel();
 
   // ---- the line: context lengths and their prefix sums -------------------------------------------------------
-  int few_b = 0, few_g = 0, few_rank = 0;
+  [[maybe_unused]] int few_b = 0, few_g = 0, few_rank = 0, few_seq = 0;
   if constexpr (kFew) {
     const int unit = blockIdx.x / p.splits;
     few_rank = blockIdx.x - unit * p.splits;
     few_b = unit / Hkv;
     few_g = unit - few_b * Hkv;
-    if (tid == 0) {
-      int len = max(0, min(p.context_lens[few_b], p.max_blocks_per_seq * kBlockSize));
+    auto set = [&](int len) {
       gaps[few_b] = window_gap(len - p.window, p.sinks);
       lens[few_b] = len - gaps[few_b] * kBlockSize;
+    };
+    auto clamped = [&](int len) { return max(0, min(len, p.max_blocks_per_seq * kBlockSize)); };
+    if constexpr (!kRuns) {
+      if (tid == 0) set(clamped(p.context_lens[few_b]));
+    } else {
+      // The row is a query token, which sees its sequence's context up to itself.
+      if (tid == 0) { misc[0] = -1; set(0); }
+      __syncthreads();
+      for (int b = tid; b < p.sequences; b += C::kThreads) {
+        const int first = p.cu_q_lens[b], end = p.cu_q_lens[b + 1], len = p.context_lens[b];
+        if (few_b >= first && few_b < end) { misc[0] = b; set(max(0, clamped(len) - (end - 1 - few_b))); }
+      }
     }
     if (lane < G) (reinterpret_cast<float*>(ring + piece0_off) + lane * C::kPieceStride)[D + 1] = 0.0f;       // (a warp without blocks has nothing)
     __syncthreads();
+    if constexpr (kRuns) few_seq = misc[0];      // -1: behind the last sequence's rows
   } else {
     constexpr int kPer = (kMaxBatch + C::kThreads - 1) / C::kThreads;
     const int chunk = p.chunk_blocks > 0 ? p.chunk_blocks : kNoChunks;
@@ -645,6 +659,7 @@ paged_decode_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
   int cnt_a = 0, pos_a = 0, ids_b = 0, cnt_b = 0, g_b = 0, y_b = 0;
   auto table_at = [&](int b, int j) -> size_t {                         // block j of what is listed of a sequence
     if constexpr (kWindow) j += j >= sink_blocks(p.sinks) ? gaps[b] : 0;
+    if constexpr (kRuns) b = few_seq;
     return static_cast<size_t>(b) * p.max_blocks_per_seq + j;
   };
   auto prefetch_q = [&](int y, int b, int g) {
@@ -750,13 +765,13 @@ paged_decode_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
   if (blockIdx.x == 0) {
     if (p.plan != nullptr && tid < kPlanCtas && p.plan->status[tid] != 0) atomicCAS(p.status, 0, p.plan->status[tid]);
     // coopt_paged_chunked takes this path only for one query token per sequence: any other split of the same total is reported
-    if (p.cu_q_lens != nullptr)
+    if (!kFew && p.cu_q_lens != nullptr)
       for (int b = tid; b <= B; b += C::kThreads)
         if (p.cu_q_lens[b] != b) atomicCAS(p.status, 0, COOPT_ERR_INVALID_ARG);
   }
   // sequences with an empty context: all-zero output rows
   if constexpr (kFew) {
-    if (lens[few_b] == 0 && few_rank == 0)
+    if (lens[few_b] == 0 && few_rank == 0 && (!kRuns || few_seq >= 0))
       for (int i = tid; i < G * D / 8; i += C::kThreads)
         reinterpret_cast<uint4*>(layer(0).out + (static_cast<size_t>(few_b) * Hq + few_g * G) * D)[i] = make_uint4(0u, 0u, 0u, 0u);
   }
@@ -1230,15 +1245,15 @@ template <int D, int FMT, int L, bool kWindow>
 int launch_one(const DecodeParams& p, const LayerTable<L>& table, int grid, cudaStream_t stream) {
   using C = Cfg<D, FMT>;
   constexpr int kSmem = kWindow ? C::kWindowSmemBytes : C::kSmemBytes;
-  if (!configure_kernel_smem(reinterpret_cast<const void*>(&paged_decode_kernel<D, FMT, L, kWindow, 0>), kSmem)) return COOPT_ERR_CUDA;
-  return launch_dependent(paged_decode_kernel<D, FMT, L, kWindow, 0>, grid, C::kThreads, kSmem, stream, p, table) ? COOPT_OK : COOPT_ERR_CUDA;
+  if (!configure_kernel_smem(reinterpret_cast<const void*>(&paged_decode_kernel<D, FMT, L, kWindow, 0, false>), kSmem)) return COOPT_ERR_CUDA;
+  return launch_dependent(paged_decode_kernel<D, FMT, L, kWindow, 0, false>, grid, C::kThreads, kSmem, stream, p, table) ? COOPT_OK : COOPT_ERR_CUDA;
 }
 // A windowed call whose units all have a CTA of their own at once, kPerSm of them on an SM, or a cluster of CTAs each: see
 // kFewPerSm in the kernel, and kFewBlocks.  `done` says whether it was one.
-template <int D, int FMT, int kPerSm>
+template <int D, int FMT, int kPerSm, bool kRuns>
 int launch_few(DecodeParams p, const LayerTable<1>& table, int listed_blocks, bool& done, cudaStream_t stream) {
   using C = Cfg<D, FMT, kPerSm>;
-  const auto kernel = paged_decode_kernel<D, FMT, 1, true, kPerSm>;
+  const auto kernel = paged_decode_kernel<D, FMT, 1, true, kPerSm, kRuns>;
   const void* address = reinterpret_cast<const void*>(kernel);
   const int units = p.batch * p.num_kv_heads;
   const DeviceInfo* di = device_info();
@@ -1251,15 +1266,29 @@ int launch_few(DecodeParams p, const LayerTable<1>& table, int listed_blocks, bo
   for (int s = wanted; s > 0 && p.splits == 0; --s)
     if (units <= (s == 1 ? kPerSm * di->num_sms : clusters_at_once(address, s, C::kThreads, C::kWindowSmemBytes))) p.splits = s;
   done = listed_blocks <= (C::kFp8 ? kFewBlocks : kFewBlocksBf16) * C::kWarps * p.splits;
+  if (kRuns) {                           // query tokens: or as tiles
+    const long long blocks = static_cast<long long>((units * p.splits + di->num_sms - 1) / di->num_sms) * ((listed_blocks + p.splits - 1) / p.splits);
+    done = done && blocks * (D == 64 ? kRunRowNs64 : kRunRowNs) <= kRunNs + p.tile_blocks * kRunTileNs;
+  }
   if (!done) return COOPT_OK;
   return launch_dependent_cluster(kernel, units * p.splits, p.splits, C::kThreads, C::kWindowSmemBytes, stream, p, table) ? COOPT_OK : COOPT_ERR_CUDA;
 }
 template <int D, int FMT>
 int launch_window(const DecodeParams& p, const LayerTable<1>& table, int grid, int listed_blocks, cudaStream_t stream) {
   bool done = false;
-  int rc = launch_few<D, FMT, 1>(p, table, listed_blocks, done, stream);
-  if (!done && rc == COOPT_OK) rc = launch_few<D, FMT, 2>(p, table, listed_blocks, done, stream);
-  if (!done && rc == COOPT_OK) rc = launch_few<D, FMT, 3>(p, table, listed_blocks, done, stream);
+  auto few = [&](auto runs) {
+    int rc = launch_few<D, FMT, 1, runs()>(p, table, listed_blocks, done, stream);
+    if (!done && rc == COOPT_OK) rc = launch_few<D, FMT, 2, runs()>(p, table, listed_blocks, done, stream);
+    if (!done && rc == COOPT_OK) rc = launch_few<D, FMT, 3, runs()>(p, table, listed_blocks, done, stream);
+    return rc;
+  };
+  if constexpr (FMT != COOPT_KV_BF16) {
+    if (p.cu_q_lens != nullptr) {
+      const int rc = few(std::true_type{});
+      return !done && rc == COOPT_OK ? kNotTaken : rc;
+    }
+  }
+  const int rc = few(std::false_type{});
   return done || rc != COOPT_OK ? rc : launch_one<D, FMT, 1, true>(p, table, grid, stream);
 }
 
@@ -1393,6 +1422,8 @@ int launch_decode(const DecodeCall& a, cudaStream_t stream) {
   p.block_table = a.block_table;
   p.context_lens = a.context_lens;
   p.cu_q_lens = a.cu_q_lens;
+  p.sequences = a.sequences;
+  p.tile_blocks = a.tile_blocks;
   p.max_blocks_per_seq = a.max_blocks_per_seq;
   p.batch = a.batch;
   p.num_q_heads = a.num_q_heads;

@@ -52,6 +52,13 @@ constexpr int kSoloShare = 48, kSoloMost = 12;
 // (All units long: 50 sequences, 8 kv heads, head_dim 128, window 2048, 33 blocks a warp, 39.2 us so, 44.7 in a line; one of 4100
 // tokens among 143 of 100: 23.7, in a line 15.)
 constexpr int kFewBlocks = 24, kFewBlocksBf16 = 36;
+// Runs of query tokens as rows of a windowed call, a unit for every token and kv head: each reads its window by itself, which the
+// prefill kernel does once for a tile of 128 / G tokens, but without that kernel's set-up (kRunNs less), and spread over more CTAs.
+// So where the units are few as above it is the blocks that decide, those that fall to an SM as rows and those that a CTA of the
+// prefill kernel goes through, at what one was measured to take, in ns.  (Prefill kernel / rows, us: 24 runs of 1..5, 16 heads over
+// 2, window 777, 16.5 / 11.3; one of 8, 40 over 8, 11.1 / 10.2; head_dim 128, 16 heads over 2, window 4000: 24 runs of 3 35.2 / 25.4,
+// one of 20 18.0 / 14.5, 8 of 8 20.0 / 25.4; head_dim 64, 16 over 4, one of 20, window 777 9.6 / 9.0, 4000 13.9 / 18.4.)
+constexpr int kRunNs = 2800, kRunTileNs = 220, kRunRowNs = 75, kRunRowNs64 = 50;
 constexpr int kNoChunks = 1 << 30;    // "blocks per chunk" of a call without chunks
 
 // A plan: header, the clamped context lengths int32[batch] (padded to 16 bytes), the block table
@@ -108,6 +115,9 @@ struct DecodeParams {
   const int* context_lens;
   const PlanHeader* plan;  // null: block_table and context_lens are the caller's own and are checked here
   const int* cu_q_lens;    // chunk mode of coopt_paged_chunked: prefix sums of the query tokens (must be 0..batch); else null
+                           // (windowed call: of the query tokens of `sequences` sequences, which are the `batch` rows)
+  int sequences;
+  long long tile_blocks;   // (host side) with them: blocks that a CTA of the prefill kernel would go through
   int plan_key;
   long long kv_token_stride;
   int layers;
@@ -151,12 +161,15 @@ struct DecodeCall {
   int64_t kv_token_stride;
   int32_t max_blocks_per_seq, batch, num_q_heads, chunk_size;
   int32_t window, sinks;            // window 0: the whole context
+  int32_t sequences;                // windowed, with cu_q_lens: rows (batch) are query tokens of so many sequences,
+  int64_t tile_blocks;              // .. which the prefill kernel would serve with CTAs of so many blocks: kNotTaken if that is faster
   float sm_scale;
   void* workspace;
   int shares;                       // decode_shares()
   int num_sms;
   DecodeOrder order;
 };
+constexpr int kNotTaken = 1;       // launch_decode for rows of several sequences: nothing was enqueued, the prefill kernel is due
 int launch_decode(const DecodeCall& a, cudaStream_t stream);
 int launch_decode_plan(const int32_t* block_table, int32_t max_blocks_per_seq, const int32_t* context_lens, int32_t batch,
                        int32_t num_kv_heads, int32_t num_blocks, int32_t chunk_size, void* plan, cudaStream_t stream);

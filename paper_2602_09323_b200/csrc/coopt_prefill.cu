@@ -889,13 +889,9 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
 }
 
 template <int D, bool kE5m2, bool kWindow>
-int launch_one(const coopt_cache* c, PrefillParams p, long long pairs, long long likely, long long key_tiles, cudaStream_t stream) {
+int launch_one(const coopt_cache* c, PrefillParams p, long long pairs, long long likely, long long key_tiles, DecodeCall* rows, cudaStream_t stream) {
   using C = Cfg<D>;
-  CUtensorMap map_part, map_hdr;
-  const long long granules = static_cast<long long>(c->num_blocks) * c->num_kv_heads;
-  if (!encode_cache_map(&map_part, c->data, granules, C::kGran, C::kPart / 8) || !encode_cache_map(&map_hdr, c->data, granules, C::kGran, kFp8Header / 8))
-    return COOPT_ERR_CUDA;
-  auto launch = [&](auto* kernel) {
+  auto launch = [&](auto* kernel) -> int {
     if (!configure_kernel_smem(reinterpret_cast<const void*>(kernel), C::kSmemBytes)) return COOPT_ERR_CUDA;
     // Where the tiles leave room on the device, the keys of one are shared out to a cluster, as large as fits for all of them at
     // once.  (n = 4 new tokens behind 9000, 40 heads over 8, head_dim 128, us with 1 / 2 / 3 / 5 / 8 CTAs: one sequence, window
@@ -904,6 +900,16 @@ int launch_one(const coopt_cache* c, PrefillParams p, long long pairs, long long
     if (kWindow && p.tiles == 1 && key_tiles > 2)
       for (int s = static_cast<int>(std::min<long long>(key_tiles, kMaxSplits)); s > 1 && p.splits == 1; --s)
         if (likely <= clusters_at_once(reinterpret_cast<const void*>(kernel), s, kThreads, C::kSmemBytes)) p.splits = s;
+    if (kWindow && rows != nullptr) {    // few tokens: perhaps better as rows of the decode kernel
+      const long long listed = std::min(p.max_blocks_per_seq, sink_blocks(p.sinks) + p.window / kBlockSize + 2);
+      rows->tile_blocks = (likely * p.splits + rows->num_sms - 1) / rows->num_sms * ((listed + p.splits - 1) / p.splits);
+      const int rc = launch_decode(*rows, stream);
+      if (rc != kNotTaken) return rc;
+    }
+    CUtensorMap map_part, map_hdr;
+    const long long granules = static_cast<long long>(c->num_blocks) * c->num_kv_heads;
+    if (!encode_cache_map(&map_part, c->data, granules, C::kGran, C::kPart / 8) || !encode_cache_map(&map_hdr, c->data, granules, C::kGran, kFp8Header / 8))
+      return COOPT_ERR_CUDA;
     if (pairs * c->num_kv_heads * p.splits > 0x7fffffffll) return COOPT_ERR_UNSUPPORTED;
     const dim3 grid(static_cast<unsigned>(pairs * c->num_kv_heads * p.splits));
     return launch_dependent_cluster(kernel, grid, kWindow ? p.splits : 1, kThreads, C::kSmemBytes, stream, p, map_part, map_hdr) ? COOPT_OK : COOPT_ERR_CUDA;
@@ -916,7 +922,7 @@ int launch_one(const coopt_cache* c, PrefillParams p, long long pairs, long long
 int launch_paged_prefill(const coopt_cache* c, const void* q, void* out, const int32_t* cu_q_lens,
                          const int32_t* block_table, int32_t max_blocks_per_seq, const int32_t* context_lens,
                          int32_t batch, int32_t num_q_heads, int32_t total_q, int32_t causal, int32_t window, int32_t sinks,
-                         float sm_scale, void* workspace, int num_sms, cudaStream_t stream) {
+                         float sm_scale, void* workspace, int num_sms, cudaStream_t stream, DecodeCall* rows) {
   if (!is_fp8(c->dtype)) return COOPT_ERR_UNSUPPORTED;
   if (c->dtype == COOPT_KV_FP8_E5M2 && c->head_dim != 128 && window == 0) return COOPT_ERR_UNSUPPORTED;
   PrefillParams p;
@@ -949,18 +955,18 @@ int launch_paged_prefill(const coopt_cache* c, const void* q, void* out, const i
   // What decides on sharing the keys of a tile out (launch_one): query tiles there will probably be, where runs are short one a
   // sequence, and tiles of keys that one of them goes through at most.
   long long likely = 0, key_tiles = 0;
-  if (window > 0 && p.tiles == 1) {
-    likely = (2ll * total_q <= static_cast<long long>(batch) * p.tile_queries ? batch : most(1)) * c->num_kv_heads;
+  if (window > 0) {
+    likely = (2ll * total_q <= static_cast<long long>(batch) * p.tile_queries ? batch : most(p.tiles)) * c->num_kv_heads;
     const long long keys = static_cast<long long>(window) + sinks + p.tile_queries + 2 * kBlockSize;
     key_tiles = (std::min(keys, static_cast<long long>(max_blocks_per_seq) * kBlockSize) + kTileKeys - 1) / kTileKeys;
   }
   const bool e5m2 = c->dtype == COOPT_KV_FP8_E5M2;
   if (window > 0) {
-    if (c->head_dim == 64) return e5m2 ? launch_one<64, true, true>(c, p, pairs, likely, key_tiles, stream) : launch_one<64, false, true>(c, p, pairs, likely, key_tiles, stream);
-    return e5m2 ? launch_one<128, true, true>(c, p, pairs, likely, key_tiles, stream) : launch_one<128, false, true>(c, p, pairs, likely, key_tiles, stream);
+    if (c->head_dim == 64) return e5m2 ? launch_one<64, true, true>(c, p, pairs, likely, key_tiles, rows, stream) : launch_one<64, false, true>(c, p, pairs, likely, key_tiles, rows, stream);
+    return e5m2 ? launch_one<128, true, true>(c, p, pairs, likely, key_tiles, rows, stream) : launch_one<128, false, true>(c, p, pairs, likely, key_tiles, rows, stream);
   }
-  if (c->head_dim == 64) return launch_one<64, false, false>(c, p, pairs, likely, key_tiles, stream);
-  return e5m2 ? launch_one<128, true, false>(c, p, pairs, likely, key_tiles, stream) : launch_one<128, false, false>(c, p, pairs, likely, key_tiles, stream);
+  if (c->head_dim == 64) return launch_one<64, false, false>(c, p, pairs, likely, key_tiles, rows, stream);
+  return e5m2 ? launch_one<128, true, false>(c, p, pairs, likely, key_tiles, rows, stream) : launch_one<128, false, false>(c, p, pairs, likely, key_tiles, rows, stream);
 }
 
 }  // namespace coopt

@@ -360,6 +360,22 @@ def test_prefill_of_several_rounds(group, hkv, batch, most, context, window, sin
     check(out, ref, spread, "e4m3", prefill=True, vmax=6.0)
 
 
+@pytest.mark.parametrize("batch,hkv,most,window,fmt,dim", [(1, 2, 6, 500, "e4m3", 128), (4, 8, 3, 900, "e5m2", 128), (12, 8, 5, 300, "e4m3", 64), (20, 4, 6, 200, "e5m2", 64),
+                                                           (150, 1, 3, 100, "e4m3", 128), (40, 8, 2, 120, "e4m3", 128), (400, 1, 1, 60, "e4m3", 64), (3, 1, 60, 40, "e5m2", 128)])
+def test_prefill_of_short_runs(batch, hkv, most, window, fmt, dim):
+    """A few new tokens a sequence (drafts to verify, tails of prompts), from one run to hundreds, empty ones and ones longer than
+    their context among them."""
+    rng = np.random.default_rng(batch + most)
+    q_lens = [int(x) for x in rng.integers(0, most + 1, batch)]
+    q_lens[-1] = most
+    lens = [max(0, n + int(x)) for n, x in zip(q_lens, rng.integers(-1, 2 * window, batch))]
+    lens[0] = 2 * window + 37
+    w, cache, kv, table = make(lens, q_lens, 3 * hkv, hkv, dim, fmt, window, 5, seed=71 + batch)
+    out = prefill(w, cache, table, window, 5, extra_rows=3)
+    ref, spread = attention.window_attention(w.q.float().numpy(), kv, w.block_table.numpy(), lens, window, 5, w.cu_q_lens.numpy())
+    check(out, ref, spread, fmt, prefill=True, vmax=6.0)
+
+
 @pytest.mark.parametrize("lens,q_lens", [([403, 64], [4, 3]), ([403, 64], [40, 30]), ([3000, 64], [200, 3]), ([700, 90] * 80, [30, 9] * 80)])
 def test_a_key_that_is_nan_reaches_those_who_see_it_and_no_one_else(lens, q_lens):
     """The last token's key of kv head 0, in each of the ways that a run is served."""
