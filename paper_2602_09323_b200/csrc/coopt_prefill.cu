@@ -30,6 +30,7 @@
 //   warps 12, 13     issue the matrix instructions of tile 0, of tile 1
 //   warp 14          copies: gather requests over the tensor map of the cache
 //   warp 15          what the softmax needs of a tile's block scales, worked out once for all rows
+// (A small CTA has 256 threads, one tile and 256 columns: Cfg.)
 //
 // Measured: 8 sequences of 4096 cached and 512 new tokens, 40 query heads over 8 kv heads, head_dim 128: 385 us (one tile a CTA,
 // its key tiles taken in turns by two groups of eight warps: 690; the two tiles' exponentials side by side and one fp32
@@ -51,8 +52,6 @@ namespace coopt {
 namespace {
 
 constexpr int kRows = 128;
-constexpr int kThreads = 512;
-constexpr int kWidenWarp = 8, kMmaWarp = 12, kCopyWarp = 14;      // warp 15: scales
 constexpr int kTileBlocks = 8;
 constexpr int kTileKeys = kTileBlocks * kBlockSize;        // 128: what is copied and widened at a time
 constexpr int kHalf = kTileKeys / 2;                       // 64: what is multiplied at a time
@@ -79,26 +78,34 @@ struct PrefillParams {
   int* status;
 };
 
-template <int D>
+// kSmall: a CTA of half the size, with one tile, two of which fit an SM: four softmax warps, two that widen, one for the matrix
+// instructions, which works the block scales out on the way, one for the copies.
+template <int D, bool kSmall = false>
 struct Cfg {
+  static constexpr int kTilesMost = kSmall ? 1 : 2;
+  static constexpr int kThreads = kSmall ? 256 : 512;
+  static constexpr int kSoftmaxWarps = 4 * kTilesMost, kWidenWarp = kSoftmaxWarps, kWidenWarps = kSmall ? 2 : 4;
+  static constexpr int kMmaWarp = kWidenWarp + kWidenWarps, kCopyWarp = kMmaWarp + kTilesMost;      // and a warp for the scales, if there is one more
+  static constexpr int kTmemColumns = kSmall ? 256 : 512;
   static constexpr bool kWideK = D == 64;                         // K is widened to f16 too
   static constexpr int kPart = kBlockSize * D;                    // K (or V) codes of one granule
   static constexpr int kGran = granule_bytes(D, true);
   static constexpr int kCodes = kTileBlocks * kPart;              // K (or V) codes of a tile
   static constexpr int kKSlot = kCodes + kTileBlocks * kFp8Header;   // K parts, then the eight headers
-  static constexpr int kKSlots = D == 128 ? 3 : 2, kVSlots = 2, kWide = 2, kScaleSlots = 4;
+  static constexpr int kKSlots = D == 128 ? 3 : 2, kVSlots = 2, kWide = 2, kScaleSlots = kSmall ? 2 : 4;
   static constexpr int kOperand = 128 * D * 2;                    // Q of a tile (two terms of codes, or f16); V^T, or K, of a tile in f16
   static constexpr int kKOff = 0;
   static constexpr int kVOff = kKOff + kKSlots * kKSlot;
   static constexpr int kQOff = kVOff + kVSlots * kCodes;
-  static constexpr int kV16Off = kQOff + 2 * kOperand;
+  static constexpr int kV16Off = kQOff + kTilesMost * kOperand;
   static constexpr int kK16Off = kV16Off + kWide * kOperand;
   static constexpr int kScaleOff = kK16Off + (kWideK ? kWide * kOperand : 0);   // [slot][32]: K scales, log2 of V scale ratios, their inverses, factor, reference
   static constexpr int kBarOff = kScaleOff + kScaleSlots * 128;
-  static constexpr int kNumBars = 2 * kKSlots + 2 * kVSlots + 4 * kWide + kScaleSlots + 21;
+  static constexpr int kNumBars = 2 * kKSlots + 2 * kVSlots + 4 * kWide + 6 * kTilesMost + 1 + (kSmall ? 0 : kScaleSlots + 8);
   static constexpr int kMiscOff = kBarOff + kNumBars * 8;
-  static constexpr int kSmemBytes = kMiscOff + 64;
-  static_assert(kKSlot % 128 == 0 && kVOff % 128 == 0 && kQOff % 128 == 0 && kSmemBytes <= 232448, "shared memory of one CTA");
+  static constexpr int kSmemBytes = kMiscOff + 32;
+  static_assert(kKSlot % 128 == 0 && kVOff % 128 == 0 && kQOff % 128 == 0 && kSmemBytes <= (kSmall ? 115712 : 232448), "shared memory of one CTA");
+  static_assert(!kSmall || kWideK, "a small CTA's K is free once it has been widened");
 };
 
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
@@ -155,11 +162,12 @@ __device__ __forceinline__ void arrive_one(uint64_t* bar) {
 // kWindow: a query sees only the last `window` tokens up to itself and the first `sinks` ones.  The CTA goes through the blocks that
 // any of its queries sees, and counts keys as if the others were not there (window_gap); what is left of the rule are masks at
 // the window's lower edge.
-template <int D, bool kE5m2, bool kTurns, bool kWindow>
-__global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const PrefillParams p, const __grid_constant__ CUtensorMap map_part,
-                                                                    const __grid_constant__ CUtensorMap map_hdr) {
-  using C = Cfg<D>;
-  constexpr bool kSplit = kWindow && !kTurns;
+template <int D, bool kE5m2, bool kTurns, bool kWindow, bool kSmall>
+__global__ void __launch_bounds__(Cfg<D, kSmall>::kThreads, kSmall ? 2 : 1)
+paged_prefill_kernel(const PrefillParams p, const __grid_constant__ CUtensorMap map_part, const __grid_constant__ CUtensorMap map_hdr) {
+  using C = Cfg<D, kSmall>;
+  constexpr int kMmaWarp = C::kMmaWarp, kCopyWarp = C::kCopyWarp;
+  constexpr bool kSplit = kWindow && !kTurns && !kSmall;
   extern __shared__ __align__(128) uint8_t smem[];
   float* scales = reinterpret_cast<float*>(smem + C::kScaleOff);
   uint64_t* bar_kfull = reinterpret_cast<uint64_t*>(smem + C::kBarOff);   // K parts and headers of a tile have landed
@@ -171,11 +179,11 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
   uint64_t* bar_k16full = bar_v16free + C::kWide;       // the same of K
   uint64_t* bar_k16free = bar_k16full + C::kWide;
   uint64_t* bar_scale = bar_k16free + C::kWide;         // the softmax's share of a tile's scales is ready
-  uint64_t* bar_sfull = bar_scale + C::kScaleSlots;     // [tile][buffer] logits of a half are in tensor memory (and the tile's scales ready)
-  uint64_t* bar_pfull = bar_sfull + 4;                  // [tile][buffer] its probabilities are, in their place
-  uint64_t* bar_pv = bar_pfull + 4;                     // [tile] its product with V is done
-  uint64_t* bar_out = bar_pv + 2;                       // [tile] .. and it was the tile's last
-  uint64_t* bar_q = bar_out + 2;                        // the query operands are in shared memory
+  uint64_t* bar_sfull = bar_scale + (kSmall ? 0 : C::kScaleSlots);     // [tile][buffer] logits of a half are in tensor memory (and the tile's scales ready)
+  uint64_t* bar_pfull = bar_sfull + 2 * C::kTilesMost;                  // [tile][buffer] its probabilities are, in their place
+  uint64_t* bar_pv = bar_pfull + 2 * C::kTilesMost;                     // [tile] its product with V is done
+  uint64_t* bar_out = bar_pv + C::kTilesMost;                       // [tile] .. and it was the tile's last
+  uint64_t* bar_q = bar_out + C::kTilesMost;                        // the query operands are in shared memory
   uint64_t* bar_turn = bar_q + 1;                       // [tile][scheduler] the exponentials of a half are done
   int* misc = reinterpret_cast<int*>(smem + C::kMiscOff);   // [0] sequence, [1] first query, [2] abort flag, [3] tensor memory, [4] first row, [5] rows, [6] context of the sequence, [7] kv head
   volatile int* abort_flag = misc + 2;
@@ -187,21 +195,21 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
 
   if (tid == 0) {
     *abort_flag = 0;
-    for (int i = 0; i < C::kKSlots; ++i) { mbar_init(&bar_kfull[i], 1); mbar_init(&bar_kfree[i], C::kWideK ? 5 : 3); }
-    for (int i = 0; i < C::kVSlots; ++i) { mbar_init(&bar_vfull[i], 1); mbar_init(&bar_vfree[i], 4); }
+    for (int i = 0; i < C::kKSlots; ++i) { mbar_init(&bar_kfull[i], 1); mbar_init(&bar_kfree[i], C::kWideK ? C::kWidenWarps + 1 : 3); }
+    for (int i = 0; i < C::kVSlots; ++i) { mbar_init(&bar_vfull[i], 1); mbar_init(&bar_vfree[i], C::kWidenWarps); }
     for (int i = 0; i < C::kWide; ++i) {
-      mbar_init(&bar_v16full[i], 4); mbar_init(&bar_v16free[i], 2);
-      mbar_init(&bar_k16full[i], 4); mbar_init(&bar_k16free[i], 2);
+      mbar_init(&bar_v16full[i], C::kWidenWarps); mbar_init(&bar_v16free[i], C::kTilesMost);
+      mbar_init(&bar_k16full[i], C::kWidenWarps); mbar_init(&bar_k16free[i], C::kTilesMost);
     }
-    for (int i = 0; i < C::kScaleSlots; ++i) mbar_init(&bar_scale[i], 1);
-    mbar_init(bar_q, 8);
-    for (int i = 0; i < 8; ++i) mbar_init(&bar_turn[i], 1);
-    for (int i = 0; i < 4; ++i) { mbar_init(&bar_sfull[i], 2); mbar_init(&bar_pfull[i], 4); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&bar_pv[i], 1); mbar_init(&bar_out[i], 1); }
+    for (int i = 0; i < C::kScaleSlots && !kSmall; ++i) mbar_init(&bar_scale[i], 1);
+    mbar_init(bar_q, C::kSoftmaxWarps);
+    for (int i = 0; i < 8 && !kSmall; ++i) mbar_init(&bar_turn[i], 1);
+    for (int i = 0; i < 2 * C::kTilesMost; ++i) { mbar_init(&bar_sfull[i], 2); mbar_init(&bar_pfull[i], 4); }
+    for (int i = 0; i < C::kTilesMost; ++i) { mbar_init(&bar_pv[i], 1); mbar_init(&bar_out[i], 1); }
     mbar_fence_init();
   }
   if (warp == kMmaWarp) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(C::kTmemColumns) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   if (tid == kCopyWarp * 32) {
@@ -315,7 +323,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
   const int kv_end = key1 - key0;
   const int n_blocks = (kv_end + kBlockSize - 1) / kBlockSize, n_tiles = (kv_end + kTileKeys - 1) / kTileKeys;
 
-  const bool live = x < 2 && qi < tile_queries(x);
+  const bool live = x < C::kTilesMost && qi < tile_queries(x);
   const size_t grow = static_cast<size_t>(row_base + q0 + x * TQ + (live ? qi : 0)) * Hq + g * G + (live ? qh : 0);
   uint32_t pend_mask = 0, pend_par = 0;                 // copy lane: the latest phase expected of every slot it has filled
 
@@ -323,11 +331,11 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
     // no such tile, or nothing visible: all-zero rows
     if (live)
       for (int d = 0; d < D; d += 8) *reinterpret_cast<uint4*>(p.out + grow * D + d) = make_uint4(0u, 0u, 0u, 0u);
-  } else if (warp < 8) {
+  } else if (warp < C::kSoftmaxWarps) {
     // ================= softmax: one row per thread ===================================================================
     asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
     const uint32_t lane_base = static_cast<uint32_t>(warp & 3) * 32u << 16;
-    const uint32_t s_cols = tmem + 2 * kHalf * x + lane_base, o_cols = tmem + 4 * kHalf + D * x + lane_base;
+    const uint32_t s_cols = tmem + 2 * kHalf * x + lane_base, o_cols = tmem + C::kTilesMost * 2 * kHalf + D * x + lane_base;
     // ---- the query operand of the warp's 32 rows, eight at a time: a lane has every fourth 16 bytes of one of them.  The bf16
     // rows come into the operand's own place first.  (Loops that are not unrolled: code that a CTA runs once is bound by the
     // fetch of its instructions, about four cycles each.  A row per lane and all of it unrolled: 12,000 cycles, head_dim 64
@@ -570,10 +578,12 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
     } else if (lane == 0) {
       atomicCAS(p.status, 0, COOPT_ERR_TIMEOUT);
     }
-  } else if (warp < kMmaWarp) {
-    // ================= widening ==========================================================================================
+  } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-    const int wt = tid - kWidenWarp * 32;
+    if (warp < kMmaWarp) {
+    // ================= widening ==========================================================================================
+    const int wt = tid - C::kWidenWarp * 32;
+    constexpr int kStep = C::kWidenWarps * 32;
     bool ok = true;
 #pragma unroll 1
     for (int t = 0; t < n_tiles && ok; ++t) {
@@ -590,7 +600,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
         const uint8_t* src = smem + C::kKOff + ks * C::kKSlot;
         uint8_t* dst = smem + C::kK16Off + w2 * C::kOperand;
 #pragma unroll 1
-        for (int i = wt; i < nb * D; i += 128) {
+        for (int i = wt; i < nb * D; i += kStep) {
           const int tok = i & 7, c = (i >> 3) % (D / 16), grp = (i >> 3) / (D / 16);
           const uint4 v = *reinterpret_cast<const uint4*>(src + grp * 8 * D + c * 128 + tok * 16);
           const uint2 a = widen4<kE5m2>(v.x), e = widen4<kE5m2>(v.y), f = widen4<kE5m2>(v.z), h = widen4<kE5m2>(v.w);
@@ -615,7 +625,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
       // (window: of the keys that no query of this CTA sees, too)
       [[maybe_unused]] const int hide = sinks - t * kTileKeys, show = window_first - t * kTileKeys;
 #pragma unroll 1
-      for (int c = wt / D; c < nb; c += 128 / D) {
+      for (int c = wt / D; c < nb; c += kStep / D) {
         const uint4 v = *reinterpret_cast<const uint4*>(src + c * C::kPart);
         uint32_t w[4] = {v.x, v.y, v.z, v.w};
         if constexpr (kWindow) {
@@ -642,8 +652,39 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
       if (lane == 0) { mbar_arrive(&bar_v16full[w2]); mbar_arrive(&bar_vfree[vs]); }
     }
     if (!ok && lane == 0) atomicCAS(p.status, 0, COOPT_ERR_TIMEOUT);
-  } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    } else {
+    // The block scales of a tile, as the softmax uses them.
+    auto make_scales = [&](int t, float& v_ref) {
+      const int ks = t % C::kKSlots;
+      if (!__all_sync(0xffffffffu, wait_bar(&bar_kfull[ks], (t / C::kKSlots) & 1u, abort_flag))) return false;
+      const int nb = min(kTileBlocks, n_blocks - t * kTileBlocks);
+      float sk = 0.0f, sv = 0.0f;
+      if (lane < nb) {
+        const float2 h = *reinterpret_cast<const float2*>(smem + C::kKOff + ks * C::kKSlot + C::kCodes + lane * kFp8Header);
+        sk = h.x; sv = h.y;
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bar_kfree[ks]);
+      const float v_tile = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(sv)));   // scales are not negative
+      float factor = 1.0f;
+      if (v_tile > v_ref * kScaleLag) {
+        factor = v_ref > 0.0f ? v_ref / v_tile : 0.0f;
+        v_ref = v_tile;
+      }
+      // (a slot is free again four tiles on: the K slots behind its tile's are handed out only once these scales have been used)
+      float* sc = scales + (t & (C::kScaleSlots - 1)) * 32;
+      const float pv = fmaxf(v_ref > 0.0f ? sv / v_ref : 0.0f, 0x1p-24f);
+      if (lane < kTileBlocks) {
+        float lg;
+        asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(lg) : "f"(pv));
+        sc[lane] = sk;
+        sc[8 + lane] = lg;
+        sc[16 + lane] = 1.0f / pv;
+        if (lane == 0) { sc[24] = factor; sc[25] = v_ref; }
+      }
+      __syncwarp();
+      return true;
+    };
     if (warp < kCopyWarp) {
       // ================= matrix instructions of one tile =================================================================
       {
@@ -656,9 +697,10 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
         const uint64_t desc_k = umma_desc(smem_u32(smem + (C::kWideK ? C::kK16Off : C::kKOff)), 128, kRowGroup);
         const uint64_t desc_q = umma_desc(smem_u32(smem + C::kQOff + mx * C::kOperand), 128, kRowGroup);
         const uint64_t desc_v = umma_desc(smem_u32(smem + C::kV16Off), 128, 2048);
-        const uint32_t s_cols = tmem + 2 * kHalf * mx, o_cols = tmem + 4 * kHalf + D * mx;
+        const uint32_t s_cols = tmem + 2 * kHalf * mx, o_cols = tmem + C::kTilesMost * 2 * kHalf + D * mx;
         const int keys = tile_keys(mx), halves = (keys + kHalf - 1) / kHalf, my_tiles = (keys + kTileKeys - 1) / kTileKeys;
         bool ok = true;
+        [[maybe_unused]] float v_ref = 0.0f;
         int done = 0;                                     // halves whose product with V has been seen to be done
         auto see_products = [&](int upto) {
           for (; ok && done < upto; ++done) {
@@ -670,7 +712,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
         auto issue_logits = [&](int h) {
           const int t = h >> 1, ks = t % kSlots;
           if ((h & 1) == 0) {
-            ok = ok && wait_warp(&bar_scale[t & (C::kScaleSlots - 1)], (t / C::kScaleSlots) & 1u, abort_flag);
+            if constexpr (kSmall) ok = ok && make_scales(t, v_ref);
+            else ok = ok && wait_warp(&bar_scale[t & (C::kScaleSlots - 1)], (t / C::kScaleSlots) & 1u, abort_flag);
             ok = ok && wait_warp(&k_full[ks], (t / kSlots) & 1u, abort_flag);
           }
           if (!ok) return;
@@ -787,43 +830,15 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
       }
       if (!ok && lane == 0) atomicCAS(p.status, 0, COOPT_ERR_TIMEOUT);
     } else {
-      // ================= block scales, as the softmax uses them =============================================================
+      // ================= block scales ======================================================================================
       float v_ref = 0.0f;
       bool ok = true;
-      for (int t = 0; t < n_tiles; ++t) {
-        const int ks = t % C::kKSlots;
-        ok = wait_bar(&bar_kfull[ks], (t / C::kKSlots) & 1u, abort_flag);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        const int nb = min(kTileBlocks, n_blocks - t * kTileBlocks);
-        float sk = 0.0f, sv = 0.0f;
-        if (lane < nb) {
-          const float2 h = *reinterpret_cast<const float2*>(smem + C::kKOff + ks * C::kKSlot + C::kCodes + lane * kFp8Header);
-          sk = h.x; sv = h.y;
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&bar_kfree[ks]);
-        const float v_tile = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(sv)));   // scales are not negative
-        float factor = 1.0f;
-        if (v_tile > v_ref * kScaleLag) {
-          factor = v_ref > 0.0f ? v_ref / v_tile : 0.0f;
-          v_ref = v_tile;
-        }
-        // (a slot is free again four tiles on: the K slots behind its tile's are handed out only once these scales have been used)
-        float* sc = scales + (t & (C::kScaleSlots - 1)) * 32;
-        const float pv = fmaxf(v_ref > 0.0f ? sv / v_ref : 0.0f, 0x1p-24f);
-        if (lane < kTileBlocks) {
-          float lg;
-          asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(lg) : "f"(pv));
-          sc[lane] = sk;
-          sc[8 + lane] = lg;
-          sc[16 + lane] = 1.0f / pv;
-          if (lane == 0) { sc[24] = factor; sc[25] = v_ref; }
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&bar_scale[t & (C::kScaleSlots - 1)]);
+      for (int t = 0; t < n_tiles && ok; ++t) {
+        ok = make_scales(t, v_ref);
+        if (ok && lane == 0) mbar_arrive(&bar_scale[t & (C::kScaleSlots - 1)]);
       }
       if (!ok && lane == 0) atomicCAS(p.status, 0, COOPT_ERR_TIMEOUT);
+    }
     }
   }
 
@@ -885,21 +900,21 @@ __global__ void __launch_bounds__(kThreads, 1) paged_prefill_kernel(const Prefil
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::kTmemColumns) : "memory");
 }
 
 template <int D, bool kE5m2, bool kWindow>
-int launch_one(const coopt_cache* c, PrefillParams p, long long pairs, long long likely, long long key_tiles, DecodeCall* rows, cudaStream_t stream) {
-  using C = Cfg<D>;
-  auto launch = [&](auto* kernel) -> int {
+int launch_one(const coopt_cache* c, PrefillParams p, bool small, long long pairs, long long likely, long long key_tiles, DecodeCall* rows, cudaStream_t stream) {
+  auto launch = [&](auto* kernel, auto config) -> int {
+    using C = decltype(config);
     if (!configure_kernel_smem(reinterpret_cast<const void*>(kernel), C::kSmemBytes)) return COOPT_ERR_CUDA;
     // Where the tiles leave room on the device, the keys of one are shared out to a cluster, as large as fits for all of them at
     // once.  (n = 4 new tokens behind 9000, 40 heads over 8, head_dim 128, us with 1 / 2 / 3 / 5 / 8 CTAs: one sequence, window
     // 4000 54.7 / 33.3 / 25.3 / 19.6 / 15.7, 1000 20.8 / 16.2 / 13.7 / 12.0 / 11.4, 250 11.9 / 11.4 / 10.6; eight sequences, 1000
     // 21.9 / 17.2, and 27.9 with three, which do not fit at once.  Two tiles of keys are not worth it: 10.6 / 10.9.)
-    if (kWindow && p.tiles == 1 && key_tiles > 2)
+    if (kWindow && !small && p.tiles == 1 && key_tiles > 2)
       for (int s = static_cast<int>(std::min<long long>(key_tiles, kMaxSplits)); s > 1 && p.splits == 1; --s)
-        if (likely <= clusters_at_once(reinterpret_cast<const void*>(kernel), s, kThreads, C::kSmemBytes)) p.splits = s;
+        if (likely <= clusters_at_once(reinterpret_cast<const void*>(kernel), s, C::kThreads, C::kSmemBytes)) p.splits = s;
     if (kWindow && rows != nullptr) {    // few tokens: perhaps better as rows of the decode kernel
       const long long listed = std::min(p.max_blocks_per_seq, sink_blocks(p.sinks) + p.window / kBlockSize + 2);
       rows->tile_blocks = (likely * p.splits + rows->num_sms - 1) / rows->num_sms * ((listed + p.splits - 1) / p.splits);
@@ -912,9 +927,11 @@ int launch_one(const coopt_cache* c, PrefillParams p, long long pairs, long long
       return COOPT_ERR_CUDA;
     if (pairs * c->num_kv_heads * p.splits > 0x7fffffffll) return COOPT_ERR_UNSUPPORTED;
     const dim3 grid(static_cast<unsigned>(pairs * c->num_kv_heads * p.splits));
-    return launch_dependent_cluster(kernel, grid, kWindow ? p.splits : 1, kThreads, C::kSmemBytes, stream, p, map_part, map_hdr) ? COOPT_OK : COOPT_ERR_CUDA;
+    return launch_dependent_cluster(kernel, grid, kWindow ? p.splits : 1, C::kThreads, C::kSmemBytes, stream, p, map_part, map_hdr) ? COOPT_OK : COOPT_ERR_CUDA;
   };
-  return p.tiles == 2 ? launch(&paged_prefill_kernel<D, kE5m2, true, kWindow>) : launch(&paged_prefill_kernel<D, kE5m2, false, kWindow>);
+  if constexpr (kWindow && D == 64)
+    if (small) return launch(&paged_prefill_kernel<D, kE5m2, false, kWindow, true>, Cfg<D, true>{});
+  return p.tiles == 2 ? launch(&paged_prefill_kernel<D, kE5m2, true, kWindow, false>, Cfg<D>{}) : launch(&paged_prefill_kernel<D, kE5m2, false, kWindow, false>, Cfg<D>{});
 }
 
 }  // namespace
@@ -949,8 +966,17 @@ int launch_paged_prefill(const coopt_cache* c, const void* q, void* out, const i
   // 40 heads over 8, head_dim 128: 256 new tokens behind 8000 139.5 us with two / 108.6 with one, 512 behind 8000, which
   // would be 168 CTAs, 151 with two; 8 heads over 1, 128 behind 32000 508 / 370, 2048 alone 42.1 / 32.6.)
   p.tiles = most(1) * c->num_kv_heads <= num_sms ? 1 : 2;
+  // Runs that fit one tile leave the other one of such a CTA empty.  At head_dim 64 a small CTA has one, and two of them fit an SM
+  // (head_dim 128: shared memory does not hold them).  Each widens its keys for one tile, so that windows have to be short.
+  // (24 runs, two tiles / small, us: of 30 tokens, 32 heads over 8, window 100 18.9 / 11.8, 500 28.4 / 18.9, 2000 45.1 / 40.1, 8000
+  // 101 / 110; of 100, 8 over 8, 20.9 / 13.1, 31.2 / 20.4, 66.7 / 47.6, 120 / 125.  Longer runs gain nothing: four prompts of 2000,
+  // 32 over 8, window 500 111.6 / 111.2, 2000 154 / 167.)
+  constexpr int kSmallWindow = 2048;
+  const bool small = window > 0 && c->head_dim == 64 && p.tiles == 2 && total_q <= static_cast<long long>(batch) * p.tile_queries &&
+                     std::min(static_cast<long long>(window), static_cast<long long>(max_blocks_per_seq) * kBlockSize) <= kSmallWindow;
+  if (small) p.tiles = 1;
   const long long pairs = most(p.tiles);
-  p.by_length = pairs * c->num_kv_heads > num_sms ? 1 : 0;
+  p.by_length = pairs * c->num_kv_heads > (small ? 2 : 1) * num_sms ? 1 : 0;
   p.splits = 1;
   // What decides on sharing the keys of a tile out (launch_one): query tiles there will probably be, where runs are short one a
   // sequence, and tiles of keys that one of them goes through at most.
@@ -962,11 +988,11 @@ int launch_paged_prefill(const coopt_cache* c, const void* q, void* out, const i
   }
   const bool e5m2 = c->dtype == COOPT_KV_FP8_E5M2;
   if (window > 0) {
-    if (c->head_dim == 64) return e5m2 ? launch_one<64, true, true>(c, p, pairs, likely, key_tiles, rows, stream) : launch_one<64, false, true>(c, p, pairs, likely, key_tiles, rows, stream);
-    return e5m2 ? launch_one<128, true, true>(c, p, pairs, likely, key_tiles, rows, stream) : launch_one<128, false, true>(c, p, pairs, likely, key_tiles, rows, stream);
+    if (c->head_dim == 64) return e5m2 ? launch_one<64, true, true>(c, p, small, pairs, likely, key_tiles, rows, stream) : launch_one<64, false, true>(c, p, small, pairs, likely, key_tiles, rows, stream);
+    return e5m2 ? launch_one<128, true, true>(c, p, small, pairs, likely, key_tiles, rows, stream) : launch_one<128, false, true>(c, p, small, pairs, likely, key_tiles, rows, stream);
   }
-  if (c->head_dim == 64) return launch_one<64, false, false>(c, p, pairs, likely, key_tiles, rows, stream);
-  return e5m2 ? launch_one<128, true, false>(c, p, pairs, likely, key_tiles, rows, stream) : launch_one<128, false, false>(c, p, pairs, likely, key_tiles, rows, stream);
+  if (c->head_dim == 64) return launch_one<64, false, false>(c, p, small, pairs, likely, key_tiles, rows, stream);
+  return e5m2 ? launch_one<128, true, false>(c, p, small, pairs, likely, key_tiles, rows, stream) : launch_one<128, false, false>(c, p, small, pairs, likely, key_tiles, rows, stream);
 }
 
 }  // namespace coopt

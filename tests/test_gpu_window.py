@@ -406,3 +406,17 @@ def spoil_last_key(w, cache, table, lens):
         at = idx[0, (L - 1) % 16].cuda()
         for byte in range(1 if cache.dtype != FMT["bf16"] else 2):
             raw[int(table[b, (L - 1) // 16]), 0, at + byte] = 0x7F if cache.dtype != FMT["bf16"] or byte == 1 else 0xC0
+
+
+@pytest.mark.parametrize("fmt,group,hkv,most,window", [("e4m3", 4, 8, 32, 500), ("e5m2", 1, 8, 128, 100), ("e4m3", 8, 4, 16, 2000), ("e5m2", 3, 8, 42, 1)])
+def test_prefill_of_many_runs_that_fit_a_tile(fmt, group, hkv, most, window):
+    """More tiles than SMs, most of them of a sequence each; one run needs several, one is empty, one has nothing to see."""
+    rng = np.random.default_rng(most)
+    q_lens = [int(x) for x in rng.integers(1, most + 1, 40)]
+    q_lens[3], q_lens[7], q_lens[9] = 0, most + most // 2, most
+    lens = [n + int(x) for n, x in zip(q_lens, rng.integers(0, 3 * window + 60, 40))]
+    lens[9] = 0
+    w, cache, kv, table = make(lens, q_lens, group * hkv, hkv, 64, fmt, window, 6, seed=83 + most)
+    out = prefill(w, cache, table, window, 6, extra_rows=2)
+    ref, spread = attention.window_attention(w.q.float().numpy(), kv, w.block_table.numpy(), lens, window, 6, w.cu_q_lens.numpy())
+    check(out, ref, spread, fmt, prefill=True, vmax=6.0)
