@@ -940,6 +940,8 @@ paged_decode_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
         top[0] = fmaxf(top[0], t0);
         top[1] = fmaxf(top[1], t1);
       }
+      // (a reference is -inf until a key's logit is not: windowed calls let a key that is infinite have no weight)
+      auto floor = [](float v) { return kWindow ? fmaxf(v, -FLT_MAX) : v; };
       const bool grow = C::kFp8 && sv > vref;
       if (__any_sync(0xffffffffu, t0 > m[0] + kLag || t1 > m[1] + kLag) || grow) {
         float f[2];
@@ -950,7 +952,7 @@ paged_decode_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
           t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 8));
           t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 16));
           const float mn = fmaxf(m[h], t);
-          f[h] = ex2(m[h] - mn);
+          f[h] = ex2(m[h] - floor(mn));
           m[h] = mn;
           l[h] *= f[h];
         }
@@ -964,7 +966,7 @@ paged_decode_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
 #pragma unroll
         for (int t = 0; t < D / 16; ++t) { o[t][0] *= f[0]; o[t][1] *= f[1]; o[t][2] *= f[0]; o[t][3] *= f[1]; }
       }
-      const float b0 = kShift - m[0], b1 = kShift - m[1];
+      const float b0 = kShift - floor(m[0]), b1 = kShift - floor(m[1]);
       float pr[4];
       pr[0] = ex2(x[0] + b0); pr[1] = ex2(x[1] + b1); pr[2] = ex2(x[2] + b0); pr[3] = ex2(x[3] + b1);
       l[0] += pr[0] + pr[2];

@@ -420,3 +420,24 @@ def test_prefill_of_many_runs_that_fit_a_tile(fmt, group, hkv, most, window):
     out = prefill(w, cache, table, window, 6, extra_rows=2)
     ref, spread = attention.window_attention(w.q.float().numpy(), kv, w.block_table.numpy(), lens, window, 6, w.cu_q_lens.numpy())
     check(out, ref, spread, fmt, prefill=True, vmax=6.0)
+
+
+@pytest.mark.parametrize("fmt,dim", [("bf16", 64), ("bf16", 128), ("e5m2", 64), ("e5m2", 128)])
+def test_a_key_of_minus_infinity_has_no_weight(fmt, dim):
+    """The first token, alone in its block, with logits of -inf: as if there were no sink."""
+    lens = [400, 1000, 40, 17] * 3
+    w, cache, kv, table = make(lens, [1] * len(lens), 2, 2, dim, fmt, 5, 1, seed=89)
+    raw = cache.data.view(w.num_blocks, 2, cache.granule_bytes)
+    idx = torch.from_numpy(helpers.granule_index_map(cache))
+    for b in range(len(lens)):
+        for h in range(2):
+            high = 0xFF if float(w.q[b, h, 0]) > 0 else 0x7F
+            at = int(idx[0, 0, 0])
+            if fmt == "bf16":
+                raw[int(table[b, 0]), h, at], raw[int(table[b, 0]), h, at + 1] = 0x80, high
+            else:
+                raw[int(table[b, 0]), h, at] = high & 0xFC
+    ref, spread = attention.window_attention(w.q.float().numpy(), kv, w.block_table.numpy(), lens, 5, 0)
+    check(decode(w, cache, table, lens, 5, 1), ref, spread, fmt)
+    if fmt == "e5m2":
+        check(prefill(w, cache, table, 5, 1), ref, spread, fmt, prefill=True, vmax=6.0)
