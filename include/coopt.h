@@ -371,7 +371,9 @@ int coopt_window_prefill(const coopt_cache* cache, const void* q, void* out, con
  * coopt_pages_fork -- row children[i] becomes a copy of row parents[i]: full blocks are shared (refs + 1), a last block that is
  *   partly filled is copied to a new one in every layer (both may be appended to from then on), released entries stay
  *   released, blocks reserved past the parent's length are not taken over.  Refused: rows out of range, a child whose length is not 0, a
- *   child's second mention, a parent that is a child in the same call.  num_caches 0: table and counts only.
+ *   child's second mention, a parent that is a child in the same call, a parent whose partly filled last block is not in use (no entry,
+ *   or one that names a free block or none of the pool).  Entries of full blocks that name a free block, or none of the pool, become -1
+ *   in the child and are reported, as in a compaction.  num_caches 0: table and counts only.
  * coopt_pages_release -- window 0: every block of row row_ids[i] is given back (refs - 1), its entries become -1 and its length
  *   0.  window > 0: the blocks that neither hold one of the first `sinks` tokens nor one of the last `window` ones are given
  *   back, as coopt_window_decode at this length, and any later one, does not read them.  A row named twice is released once.

@@ -64,7 +64,11 @@ class Pool:
     def fork(self, parents, children) -> None:
         rows = self.table.shape[0]
         named = set(int(c) for c in children)
-        seen, asked, free, shared, lens = set(), 0, self._free(), [], self.lens.copy()
+        seen, asked, free, shared, lens, used = set(), 0, self._free(), [], self.lens.copy(), self.refs > 0
+
+        def in_use(x):                                        # .. before the call
+            return 0 <= x < len(used) and bool(used[x])
+
         for p, c in zip(parents, children):
             p, c = int(p), int(c)
             ok = 0 <= p < rows and 0 <= c < rows and c not in seen and p not in named and lens[c] == 0
@@ -75,7 +79,10 @@ class Pool:
                 continue
             length = int(lens[p])
             row = np.full(self.table.shape[1], -1, dtype=np.int32)
-            if length % BLOCK_SIZE and self.table[p, length // BLOCK_SIZE] >= 0:
+            if length % BLOCK_SIZE:
+                if not in_use(int(self.table[p, length // BLOCK_SIZE])):
+                    self.problems.add("invalid")
+                    continue
                 asked += 1
                 if asked > free:
                     self.problems.add("pages")
@@ -85,6 +92,10 @@ class Pool:
                 self.contents[:, block] = self.contents[:, self.table[p, length // BLOCK_SIZE]]
             full = length // BLOCK_SIZE
             row[:full] = self.table[p, :full]
+            for j in range(full):
+                if row[j] >= 0 and not in_use(int(row[j])):
+                    self.problems.add("invalid")
+                    row[j] = -1
             shared += [int(x) for x in row[:full] if x >= 0]
             self.table[c], self.lens[c] = row, length
         for block in shared:

@@ -42,6 +42,7 @@ struct Plan {
   int* dst;
   int* list;               // [blocks]: free blocks in order (fork, reserve); new number of every block, -1 if free (compact)
   int* fork_len;           // [rows]: tokens that a fork takes over, -1 if it is refused
+  unsigned* used;          // [blocks / 32]: fork: the blocks in use before the call, as bits
 };
 long long plan_pairs(long long blocks, long long rows) { return blocks / 2 + 1 > rows ? blocks / 2 + 1 : rows; }
 Plan plan_of(void* workspace, int blocks, int rows) {
@@ -53,6 +54,7 @@ Plan plan_of(void* workspace, int blocks, int rows) {
   p.dst = p.src + plan_pairs(blocks, rows);
   p.list = p.dst + plan_pairs(blocks, rows);
   p.fork_len = p.list + blocks;
+  p.used = reinterpret_cast<unsigned*>(p.fork_len + rows);
   return p;
 }
 
@@ -226,6 +228,11 @@ pages_reserve_kernel(const Pool pool, const Plan plan, const int* row_ids, const
 }
 
 // ---- fork -------------------------------------------------------------------------------------------------------------
+// Only blocks in use can be shared or copied: an entry that names a free one (a table that its counts do not stand for) must
+// not raise a count, since the same call may hand that block out.  "In use" is by the counts as they were before the call: as
+// bits, since the counts change on its way.
+__device__ __forceinline__ bool is_used(const unsigned* bits, int blocks, int id) { return id >= 0 && id < blocks && ((bits[id >> 5] >> (id & 31)) & 1u) != 0; }
+
 __global__ void __cluster_dims__(kClusterCtas, 1, 1) __launch_bounds__(kPlanThreads, 1)
 pages_fork_plan_kernel(const Pool pool, const Plan plan, const int* parents, const int* children, int n) {
   extern __shared__ __align__(16) uint8_t smem[];
@@ -250,14 +257,16 @@ pages_fork_plan_kernel(const Pool pool, const Plan plan, const int* parents, con
       const int L = length(p);
       t = -1;
       if (L % kBlockSize != 0) {
+        // (the counts themselves: they change behind the cluster's last meeting)
         const int id = pool.table[static_cast<size_t>(p) * pool.width + L / kBlockSize];
-        if (id >= 0 && id < pool.blocks) t = id;
+        t = id >= 0 && id < pool.blocks && pool.refs[id] > 0 ? id : -2;
       }
     }
     if (t == -2 && rank == 0) report(plan.status, COOPT_ERR_INVALID_ARG);
     tail[i] = t;
     sum += t >= 0;
   }
+  for (int w = threadIdx.x; w < s.words; w += kPlanThreads) plan.used[s.first / 32 + w] = s.bits[w];
   rank_slice(s, warp_sums, cluster_sums);
   const int free_blocks = pool.blocks - s.used;
   int total, at = cta_scan(sum, warp_sums, total);
@@ -385,16 +394,21 @@ __device__ __forceinline__ void copy_granules(const Copies& c, int warps, int la
     copy_granule(c, c.cache[blockIdx.y], c.src[pair], c.dst[pair], t - pair * c.heads, lane);
   }
 }
-// A row of the table that a fork writes: entry j of a child whose parent holds `len` tokens.
-__device__ __forceinline__ void fork_entry(const Pool& pool, int* status, int parent, int child, int len, int tail_dst, int j) {
+// A row of the table that a fork writes: entry j of a child whose parent holds `len` tokens.  `used`: see is_used.
+__device__ __forceinline__ void fork_entry(const Pool& pool, const unsigned* used, int* status, int parent, int child, int len, int tail_dst, int j) {
   int id = -1;
   if (j < len / kBlockSize) {
     id = pool.table[static_cast<size_t>(parent) * pool.width + j];
-    if (id >= pool.blocks) {
-      report(status, COOPT_ERR_INVALID_ARG);
+    if (id >= 0) {
+      if (is_used(used, pool.blocks, id)) {
+        atomicAdd(&pool.refs[id], 1);
+      } else {
+        report(status, COOPT_ERR_INVALID_ARG);
+        id = -1;
+      }
+    } else {
       id = -1;
     }
-    if (id >= 0) atomicAdd(&pool.refs[id], 1); else id = -1;
   } else if (j * kBlockSize < len) {
     id = tail_dst;
   }
@@ -414,7 +428,7 @@ __global__ void __launch_bounds__(kCopyThreads) pages_move_kernel(const __grid_c
       for (long long t = warp; t < static_cast<long long>(w.forks) * per_row; t += warps) {
         const int i = static_cast<int>(t / per_row), j = static_cast<int>(t - static_cast<long long>(i) * per_row) * 32 + lane;
         const int len = w.plan.fork_len[i];
-        if (len >= 0 && j < pool.width) fork_entry(pool, w.plan.status, w.parents[i], w.children[i], len, w.plan.dst[i], j);
+        if (len >= 0 && j < pool.width) fork_entry(pool, w.plan.used, w.plan.status, w.parents[i], w.children[i], len, w.plan.dst[i], j);
       }
     } else {
       const int U = w.plan.header[0];
@@ -440,7 +454,7 @@ __global__ void __launch_bounds__(kCopyThreads) pages_move_kernel(const __grid_c
 // ---- fork and compaction of smaller pools, in one launch ---------------------------------------------------------------------
 // Every CTA looks through the counts and makes the whole plan for itself, in shared memory, then does its part of the work: what a
 // second launch and the way of the plan through memory would take is saved.  Nothing that a CTA writes on its way changes
-// another one's plan: blocks that are in use stay so, parents are no children.  What would (the new blocks' counts and the
+// another one's plan: only counts of blocks in use are raised (is_used), which stay so, parents are no children.  What would (the new blocks' counts and the
 // children's lengths; in place, the moved counts) is written by the CTA that has counted itself last, when all have made
 // their plans.
 // (us with a planning launch / so; release and fork of 8 rows over four layers, pool of 700 / 8000 / 30000 blocks 10.0 / 7.2, 9.9 /
@@ -513,13 +527,12 @@ __global__ void __launch_bounds__(kOneThreads, 1) pages_fork_one_kernel(const __
   const int L = rows_ok ? max(0, min(__ldcg(pool.lens + p), pool.width * kBlockSize)) : 0, old_len = rows_ok ? __ldcg(pool.lens + child) : 1;
   for (int r = threadIdx.x; r < pool.rows; r += kOneThreads) owner[r] = INT_MAX;
   int tail = L % kBlockSize != 0 ? pool.table[static_cast<size_t>(p) * pool.width + L / kBlockSize] : -1;
-  if (tail >= pool.blocks) tail = -1;
   OneSlice s;
   load_pool(pool, bits, warp_sums, s);
   if (i < n && child >= 0 && child < pool.rows) atomicMin(&owner[child], i);
   __syncthreads();
   // a child is an empty row, named once, and no parent of another
-  const bool ok = rows_ok && owner[child] == i && owner[p] == INT_MAX && old_len == 0;
+  const bool ok = rows_ok && owner[child] == i && owner[p] == INT_MAX && old_len == 0 && (L % kBlockSize == 0 || is_used(bits, pool.blocks, tail));
   if (i < n && !ok && blockIdx.x == 0) report(status, COOPT_ERR_INVALID_ARG);
   const bool copy = ok && tail >= 0;
   int total;
@@ -551,7 +564,7 @@ __global__ void __launch_bounds__(kOneThreads, 1) pages_fork_one_kernel(const __
   const int per_row = (pool.width + 31) / 32;
   for (int t = warp; t < n * per_row; t += warps) {
     const int f = t / per_row, j = (t - f * per_row) * 32 + lane;
-    if (lens[f] >= 0 && j < pool.width) fork_entry(pool, status, parents[f], children[f], lens[f], dst[f], j);
+    if (lens[f] >= 0 && j < pool.width) fork_entry(pool, bits, status, parents[f], children[f], lens[f], dst[f], j);
   }
   const unsigned granules = static_cast<unsigned>(n) * c.heads, items = granules * layers;
   for (unsigned t = place_of_warp(items, warps); t < items; t += warps) {
@@ -834,7 +847,7 @@ extern "C" {
 
 size_t coopt_pages_workspace_bytes(int32_t num_blocks, int32_t rows) {
   if (num_blocks <= 0 || rows <= 0) return 0;
-  const size_t ints = 32 + 2 * static_cast<size_t>(plan_pairs(num_blocks, rows)) + num_blocks + rows;
+  const size_t ints = 32 + 2 * static_cast<size_t>(plan_pairs(num_blocks, rows)) + num_blocks + rows + (num_blocks + 31) / 32;
   return (workspace_control_bytes() + ints * 4 + 255) / 256 * 256;
 }
 
