@@ -320,8 +320,8 @@ int coopt_decode_step_host(const coopt_cache* cache, const void* step_inputs_hos
  * (coopt_paged_chunked's causal) result.
  *   window >= 1, sinks >= 0; either may exceed the contexts.
  * A key that is NaN makes the outputs of the queries that see it NaN, and of no others; one whose logit is -inf has no weight.
- * What tokens hold that no query of the call sees does not matter; a value that is NaN in a token of a run may reach the run's
- * earlier queries (probability zero times NaN).
+ * A value that is not finite reaches, in its dim, the outputs of the queries that see its token, and of no others (a scale that is
+ * infinite: those that see a token of its block).  What tokens hold that no query of the call sees does not matter.
  *
  * coopt_window_decode -- one query token per sequence, at position context_lens[b] - 1; the arguments of coopt_paged_decode.
  *   k_new, v_new, slot_mapping  the step's new tokens, written first, as for coopt_decode_step_planned (the same precondition:

@@ -42,6 +42,8 @@
 // cycles (head_dim 64: 10,000).
 // Every wait is bounded; a wait that runs out is reported in the status word and all roles leave through the common exit,
 // which frees the tensor memory.
+#include <float.h>
+
 #include <algorithm>
 
 #include "coopt_decode.cuh"
@@ -75,6 +77,7 @@ struct PrefillParams {
   float sm_scale_log2;
   int window, sinks;       // windowed call: a query sees the `window` tokens up to itself, and the first `sinks`; else unused
   int splits;              // windowed call: CTAs (a cluster) that share the keys of one tile of queries
+  const uint8_t* cache;    // windowed call: for rows that are worked out by themselves (lone_row)
   int* status;
 };
 
@@ -122,6 +125,7 @@ __device__ __forceinline__ uint2 widen4(uint32_t w) {
   if (kE5m2) return make_uint2(e5m2x2_to_f16x2_lo(w), e5m2x2_to_f16x2_hi(w));
   return make_uint2(e4m3x2_to_f16x2_lo(w), e4m3x2_to_f16x2_hi(w));
 }
+__device__ __forceinline__ float2 f16x2_to_f32(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
 // Two fp32 operations in one instruction.
 __device__ __forceinline__ uint64_t f32_pair(float a, float b) {
   uint64_t d;
@@ -156,6 +160,80 @@ __device__ __forceinline__ void arrive_one(uint64_t* bar) {
   asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n @q mbarrier.arrive.shared::cta.b64 _, [%0];\n}" ::"r"(smem_u32(bar)) : "memory");
 }
 
+// One row (query token `at` of its sequence, one head) by one warp, from the tokens that it sees and no others: a windowed call's way
+// out for rows that the matrix products cannot have right.  A product with V takes every key of a tile of keys for every row of
+// a tile of queries, and a value that is no finite number makes zero times itself, NaN, of the rows that do not see it.  Keys 16 at a
+// time (a block): a lane has half of the dims of one key of the logits, and D / 32 dims of the result.  Scales stay outside the
+// sums, as in the decode kernel.  (Calls without such values do not get here, and pay for the look at their results alone.  A function
+// of its own, since inlined it took the loops' registers: 8 chunks behind streams 115 us, so 110, without it 112.)
+template <int D, bool kE5m2>
+__device__ __noinline__ void lone_row(const PrefillParams& p, int b, int g, size_t row, int at, int lane) {
+  constexpr int kPer = D / 32;
+  const int tok = lane & 15, c0 = (lane >> 4) * kPer;
+  const __nv_bfloat16* q = p.q + row * D;
+  const int* blocks = p.block_table + static_cast<size_t>(b) * p.max_blocks_per_seq;
+  const int first = max(0, at - p.window + 1) / kBlockSize, sinks = sink_blocks(p.sinks);
+  float m = -INFINITY, l = 0.0f, o[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) o[i] = 0.0f;
+#pragma unroll 1
+  for (int j = 0; j * kBlockSize <= at; ++j) {
+    if (j >= sinks && j < first) j = first;
+    int id = blocks[j];
+    if (id < 0 || id >= p.num_blocks) id = 0;          // (reported where it was first looked at)
+    const uint8_t* gran = p.cache + (static_cast<size_t>(id) * p.num_kv_heads + g) * granule_bytes(D, true);
+    const float2 scale = *reinterpret_cast<const float2*>(gran + header_offset(D));
+    float dot = 0.0f;
+#pragma unroll 1
+    for (int c = c0; c < c0 + kPer; ++c) {
+      const uint4 k = *reinterpret_cast<const uint4*>(gran + (tok >> 3) * 8 * D + c * 128 + (tok & 7) * 16);
+      const uint32_t w[4] = {k.x, k.y, k.z, k.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint2 h = widen4<kE5m2>(w[i]), qv = *reinterpret_cast<const uint2*>(q + 16 * c + 4 * i);
+        const float2 lo = f16x2_to_f32(h.x), hi = f16x2_to_f32(h.y);
+        dot += bf16_lo(qv.x) * lo.x + bf16_hi(qv.x) * lo.y + bf16_lo(qv.y) * hi.x + bf16_hi(qv.y) * hi.y;
+      }
+    }
+    dot += __shfl_xor_sync(0xffffffffu, dot, 16);
+    const int pos = j * kBlockSize + tok;
+    const bool sees = pos <= at && (pos < p.sinks || pos > at - p.window);
+    const float x = sees ? dot * (scale.x * p.sm_scale_log2) : -INFINITY;
+    const float top = fmaxf(m, ordered_to_f32(__reduce_max_sync(0xffffffffu, f32_to_ordered(fmaxf(x, -INFINITY))))), ref = fmaxf(top, -FLT_MAX);      // (finite while no key has a weight)
+    const float w = ex2(x - ref), keep = ex2(m - ref);
+    m = top;
+    l = l * keep + 0.5f * warp_sum(w);                 // (two lanes have every key)
+    if (isnan(l)) break;
+    float v[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) v[i] = 0.0f;
+    const unsigned seen = __ballot_sync(0xffffffffu, sees);
+#pragma unroll
+    for (int t4 = 0; t4 < 4; ++t4) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int d = lane * kPer + i;
+        const uint2 h = widen4<kE5m2>(*reinterpret_cast<const uint32_t*>(gran + kBlockSize * D + (d >> 3) * 128 + (d & 7) * 16 + 4 * t4));
+        const float2 lo = f16x2_to_f32(h.x), hi = f16x2_to_f32(h.y);
+        const float e[4] = {lo.x, lo.y, hi.x, hi.y};
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const float wt = __shfl_sync(0xffffffffu, w, 4 * t4 + t);
+          if ((seen >> (4 * t4 + t)) & 1u) v[i] += wt * e[t];
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) o[i] = o[i] * keep + v[i] * scale.y;
+  }
+  const float inv = l <= 0.0f ? 0.0f : 1.0f / l;       // (NaN stays)
+#pragma unroll
+  for (int i = 0; i < kPer; i += 2) *reinterpret_cast<uint32_t*>(p.out + row * D + lane * kPer + i) = pack_bf16x2(inv != 0.0f ? o[i] * inv : 0.0f, inv != 0.0f ? o[i + 1] * inv : 0.0f);
+}
+// The larger magnitudes of two pairs of bf16, and whether one of a pair is no finite number.
+__device__ __forceinline__ uint32_t larger_magnitudes(uint32_t so_far, uint32_t pair) { return __vmaxu2(so_far, pair & 0x7FFF7FFFu); }
+__device__ __forceinline__ bool not_finite(uint32_t pair) { return pair >= 0x7F800000u || (pair & 0xFFFFu) >= 0x7F80u; }
+
 // kTurns: the two tiles of a CTA take turns at the exponentials.  A launch with one tile a CTA has a kernel without that code, which
 // nothing waits in there but which costs all the same (256 new tokens behind 2 x 8192, G = 8, 115.4 / 113.2 us; 24 sequences of
 // 335..671 tokens, one head, 23.8 / 23.4).
@@ -164,7 +242,7 @@ __device__ __forceinline__ void arrive_one(uint64_t* bar) {
 // the window's lower edge.
 template <int D, bool kE5m2, bool kTurns, bool kWindow, bool kSmall>
 __global__ void __launch_bounds__(Cfg<D, kSmall>::kThreads, kSmall ? 2 : 1)
-paged_prefill_kernel(const PrefillParams p, const __grid_constant__ CUtensorMap map_part, const __grid_constant__ CUtensorMap map_hdr) {
+paged_prefill_kernel(const __grid_constant__ PrefillParams p, const __grid_constant__ CUtensorMap map_part, const __grid_constant__ CUtensorMap map_hdr) {
   using C = Cfg<D, kSmall>;
   constexpr int kMmaWarp = C::kMmaWarp, kCopyWarp = C::kCopyWarp;
   constexpr bool kSplit = kWindow && !kTurns && !kSmall;
@@ -325,6 +403,7 @@ paged_prefill_kernel(const PrefillParams p, const __grid_constant__ CUtensorMap 
 
   const bool live = x < C::kTilesMost && qi < tile_queries(x);
   const size_t grow = static_cast<size_t>(row_base + q0 + x * TQ + (live ? qi : 0)) * Hq + g * G + (live ? qh : 0);
+  [[maybe_unused]] unsigned again = 0;                  // softmax warps of a windowed call: those of the warp's rows that lone_row is due for
   uint32_t pend_mask = 0, pend_par = 0;                 // copy lane: the latest phase expected of every slot it has filled
 
   if (all_tiles == 0) {
@@ -567,12 +646,18 @@ paged_prefill_kernel(const PrefillParams p, const __grid_constant__ CUtensorMap 
           *reinterpret_cast<uint4*>(rows + lane * D * 2 + ((4 * c + j) ^ (lane & (kLanes - 1))) * 16) = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
       }
       __syncwarp();
+      [[maybe_unused]] unsigned odd = 0;      // rows with a result that is not finite (looked at here: on the way into shared memory it took 2 us of 129)
 #pragma unroll 4
       for (int i = 0; i < kLanes; ++i) {
         const int row = kRowsAt * i + at_row, off = __shfl_sync(0xffffffffu, row_off, row);
-        if (off >= 0)
-          *reinterpret_cast<uint4*>(p.out + (tile_row + off) * D + at * 8) = *reinterpret_cast<const uint4*>(rows + row * D * 2 + (at ^ (row & (kLanes - 1))) * 16);
+        const uint4 v = *reinterpret_cast<const uint4*>(rows + row * D * 2 + (at ^ (row & (kLanes - 1))) * 16);
+        if (off >= 0) *reinterpret_cast<uint4*>(p.out + (tile_row + off) * D + at * 8) = v;
+        if constexpr (kWindow) {
+          const uint32_t most = larger_magnitudes(larger_magnitudes(larger_magnitudes(v.x & 0x7FFF7FFFu, v.y), v.z), v.w);
+          if (not_finite(most) && off >= 0) odd |= 1u << row;
+        }
       }
+      if constexpr (kWindow) again = __reduce_or_sync(0xffffffffu, odd) & __ballot_sync(0xffffffffu, l_row < INFINITY);
       tc_fence_before();
       }
     } else if (lane == 0) {
@@ -861,9 +946,9 @@ paged_prefill_kernel(const PrefillParams p, const __grid_constant__ CUtensorMap 
         const int chunk = lane % kChunks;
         const uint32_t parts = smem_u32(smem + C::kQOff), sums = smem_u32(smem + C::kVOff);
 #pragma unroll 1
-        for (int i = warp * kAt + lane / kChunks; i < share; i += 8 * kAt) {
-          const int row = rank * share + i;
-          if (row >= rows) break;
+        for (int i0 = warp * kAt, turn = 0; i0 < share; i0 += 8 * kAt, turn += kAt) {
+          const int i = i0 + lane / kChunks, row = rank * share + i;
+          if (i >= share || row >= rows) break;
           float2 ml[kMaxSplits];
           float4 o[kMaxSplits];
           float top = -INFINITY;
@@ -890,8 +975,9 @@ paged_prefill_kernel(const PrefillParams p, const __grid_constant__ CUtensorMap 
           }
           const float inv = den > 0.0f ? 1.0f / den : 0.0f;
           const int q = row / G, h = row - q * G;
-          *reinterpret_cast<uint2*>(p.out + (static_cast<size_t>(row_base + q0 + q) * Hq + g * G + h) * D + 4 * chunk) =
-              make_uint2(pack_bf16x2(num.x * inv, num.y * inv), pack_bf16x2(num.z * inv, num.w * inv));
+          const uint2 result = make_uint2(pack_bf16x2(num.x * inv, num.y * inv), pack_bf16x2(num.z * inv, num.w * inv));
+          *reinterpret_cast<uint2*>(p.out + (static_cast<size_t>(row_base + q0 + q) * Hq + g * G + h) * D + 4 * chunk) = result;
+          if (not_finite(larger_magnitudes(result.x & 0x7FFF7FFFu, result.y)) && den < INFINITY) again |= 1u << (turn + lane / kChunks);
         }
       }
       __syncwarp();
@@ -901,6 +987,23 @@ paged_prefill_kernel(const PrefillParams p, const __grid_constant__ CUtensorMap 
   tc_fence_before();
   __syncthreads();
   if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::kTmemColumns) : "memory");
+  if constexpr (kWindow) {
+    if (warp < C::kSoftmaxWarps) {
+      const bool joined = kSplit && p.splits > 1;
+      if (joined) again = __reduce_or_sync(0xffffffffu, again);
+#pragma unroll 1
+      for (; again != 0; again &= again - 1) {
+        const int n = __ffs(again) - 1;
+        int row = 32 * (warp & 3) + n;
+        if (joined) {                    // the warp's n-th row of the CTA's share, counted as they were joined
+          constexpr int kAt = 128 / D;
+          row = blockIdx.x % p.splits * ((tile_queries(0) * G + p.splits - 1) / p.splits) + warp * kAt + n / kAt * 8 * kAt + n % kAt;
+        }
+        const int q = q0 + x * (joined ? 0 : TQ) + row / G;
+        lone_row<D, kE5m2>(p, b, g, static_cast<size_t>(row_base + q) * Hq + g * G + row % G, misc[6] - n_new + q, lane);
+      }
+    }
+  }
 }
 
 template <int D, bool kE5m2, bool kWindow>
@@ -959,6 +1062,7 @@ int launch_paged_prefill(const coopt_cache* c, const void* q, void* out, const i
   p.sm_scale_log2 = sm_scale * kLog2e;
   p.window = window;
   p.sinks = sinks;
+  p.cache = static_cast<const uint8_t*>(c->data);
   p.status = static_cast<int*>(workspace);
   auto most = [&](int tiles) { return static_cast<long long>(total_q) / (tiles * p.tile_queries) + batch; };   // every sequence adds at most one that is partly filled
   // A CTA with one tile takes about 0.73 of the time of one with two (the tensor core and the exponential units are less busy,

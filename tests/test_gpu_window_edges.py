@@ -1,0 +1,140 @@
+"""Windowed prefill where the cache holds numbers that are not finite, through each of the kernels that a run can be served by.
+
+Which kernel that was is read from the device's own record of its launches, so that a changed rule on sizes cannot leave one of them
+untested.  Tolerances are those of the windowed calls on finite caches (tests/test_gpu_window.py); a row that is worked out by itself
+has fewer roundings than the others.
+"""
+import json
+import re
+
+import numpy as np
+import pytest
+import torch
+from torch.profiler import ProfilerActivity, profile
+
+from oracle import attention
+from tests import helpers
+from tests.test_gpu_window import check, make, prefill
+
+pytestmark = pytest.mark.gpu
+
+# name: (lens, q_lens, kv heads, group, window, sinks).  More than 512 query tokens are never rows of the decode kernel; tiles
+# that leave the device's SMs room are one to a CTA, and where a window has several tiles of keys those are shared by a cluster.
+RUNS = {
+    "rows": ([403, 64, 9, 700], [4, 3, 9, 5], 2, 5, 200, 3),
+    "one tile": ([900, 700, 40], [300, 250, 40], 2, 4, 60, 3),
+    "cluster": ([1900, 700, 40], [300, 250, 40], 2, 4, 1000, 3),
+    "two tiles": ([900, 420, 300, 77] * 4, [300, 20, 300, 40] * 4, 4, 4, 150, 3),
+    "small": ([400, 33, 90] * 14, [25, 33, 17] * 14, 8, 3, 120, 3),
+}
+KERNELS = {"rows": (64, 128), "one tile": (64, 128), "cluster": (64, 128), "two tiles": (64, 128), "small": (64,)}
+ROUTES = [(name, dim) for name, dims in KERNELS.items() for dim in dims]
+
+
+def served_by(call, tmp_path):
+    """The result of a call, and which kernel gave it."""
+    with profile(activities=[ProfilerActivity.CUDA]) as prof:
+        result = call()
+        torch.cuda.synchronize()
+    path = str(tmp_path / "launches.json")
+    prof.export_chrome_trace(path)
+    with open(path) as f:
+        seen = [(e["name"], e["args"]["grid"][0]) for e in json.load(f)["traceEvents"] if e.get("cat") == "kernel"]
+    return result, [x for x in seen if "paged_" in x[0]]
+
+
+def route_of(launches, w):
+    (name, grid), = launches
+    if "paged_decode_kernel" in name:
+        assert re.search(r"true>", name), name             # rows that are query tokens
+        return "rows"
+    turns, window, small = re.search(r"paged_prefill_kernel<\d+, \w+, (\w+), (\w+), (\w+)>", name).groups()
+    assert window == "true", name
+    if small == "true":
+        return "small"
+    if turns == "true":
+        return "two tiles"
+    tile = 128 // (w.num_q_heads // w.num_kv_heads)
+    pieces = (w.q.shape[0] // tile + w.batch) * w.num_kv_heads
+    assert grid % pieces == 0
+    return "one tile" if grid == pieces else "cluster"
+
+
+def runs(name, dim, fmt, seed):
+    lens, q_lens, hkv, group, window, sinks = RUNS[name]
+    w, cache, kv, table = make(lens, q_lens, group * hkv, hkv, dim, fmt, window, sinks, seed=seed)
+    ref, spread = attention.window_attention(w.q.float().numpy(), kv, w.block_table.numpy(), lens, window, sinks, w.cu_q_lens.numpy())
+    return w, cache, table, ref, spread
+
+
+def granules(w, cache):
+    return cache.data.view(w.num_blocks, w.num_kv_heads, cache.granule_bytes), torch.from_numpy(helpers.granule_index_map(cache))
+
+
+def positions(name, w):
+    """Of every query row: its sequence and its position."""
+    lens, q_lens = RUNS[name][:2]
+    of = np.repeat(np.arange(len(lens)), q_lens)
+    at = np.concatenate([L - n + np.arange(n) for L, n in zip(lens, q_lens)])
+    return of, at
+
+
+def some_tokens(name):
+    """Per sequence, tokens that some queries of a run see and others do not: one at the window's lower edge, one in the run."""
+    lens, q_lens, _, _, window, _ = RUNS[name]
+    picked = []
+    for L, n in zip(lens, q_lens):
+        edge = L - n - window + 1 + n // 2                 # seen by the first half of the run
+        picked.append(sorted({p for p in (edge, L - n + n // 3) if 3 <= p < L}))
+    return picked
+
+
+@pytest.mark.parametrize("fmt,code", [("e4m3", 0x7F), ("e5m2", 0x7C), ("e5m2", 0xFE)])
+@pytest.mark.parametrize("name,dim", ROUTES)
+def test_a_value_that_is_not_finite_reaches_those_who_see_it_and_no_one_else(name, dim, fmt, code, tmp_path):
+    w, cache, table, ref, spread = runs(name, dim, fmt, seed=301)
+    window, sinks, group = RUNS[name][4], RUNS[name][5], RUNS[name][3]
+    raw, idx = granules(w, cache)
+    of, at = positions(name, w)
+    sees = np.zeros(len(of), dtype=bool)
+    for b, picked in enumerate(some_tokens(name)):
+        for pos in picked:
+            raw[int(table[b, pos // 16]), 1, int(idx[1, pos % 16, 5])] = code      # dim 5 of its value, kv head 1
+            sees |= (of == b) & (at >= pos) & ((at - window < pos) | (pos < sinks))
+    assert 0 < sees.sum() < len(sees)
+    out, launches = served_by(lambda: prefill(w, cache, table, window, sinks, extra_rows=2), tmp_path)
+    assert route_of(launches, w) == name
+    spoilt = out[torch.from_numpy(sees)][:, group:2 * group, 5].float()
+    assert not torch.isfinite(spoilt).any()
+    out = out.clone()
+    hit = np.zeros(ref.shape, dtype=bool)
+    hit[sees, group:2 * group, 5] = True
+    out[torch.from_numpy(hit)] = torch.from_numpy(ref[hit]).to(torch.bfloat16).cuda()
+    check(out, ref, spread, fmt, prefill=True, vmax=6.0, what=name)
+
+
+@pytest.mark.parametrize("name,dim", ROUTES)
+def test_a_value_scale_that_is_infinite_reaches_those_who_see_its_block(name, dim, tmp_path):
+    """What a token with an infinite value leaves: codes of zero under a scale that is infinite."""
+    w, cache, table, ref, spread = runs(name, dim, "e4m3", seed=303)
+    lens, q_lens, _, group, window, sinks = RUNS[name]
+    raw, idx = granules(w, cache)
+    of, at = positions(name, w)
+    sees = np.zeros(len(of), dtype=bool)
+    for b, picked in enumerate(some_tokens(name)):
+        for pos in picked[:1]:
+            blk = pos // 16
+            header = raw[int(table[b, blk]), 0, 32 * dim:32 * dim + 8].clone().view(torch.float32)
+            header[1] = float("inf")
+            raw[int(table[b, blk]), 0, 32 * dim:32 * dim + 8] = header.view(torch.uint8)
+            for t in range(16 * blk, min(16 * blk + 16, lens[b])):
+                sees |= (of == b) & (at >= t) & ((at - window < t) | (t < sinks))
+    assert sees.any() and (name == "rows" or not sees.all())      # (every token of a short run sees those blocks)
+    out, launches = served_by(lambda: prefill(w, cache, table, window, sinks), tmp_path)
+    assert route_of(launches, w) == name
+    assert not torch.isfinite(out[torch.from_numpy(sees)][:, :group].float()).any()
+    out = out.clone()
+    hit = np.zeros(ref.shape, dtype=bool)
+    hit[sees, :group] = True
+    out[torch.from_numpy(hit)] = torch.from_numpy(ref[hit]).to(torch.bfloat16).cuda()
+    check(out, ref, spread, "e4m3", prefill=True, vmax=6.0, what=name)
