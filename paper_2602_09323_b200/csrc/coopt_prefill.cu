@@ -162,7 +162,9 @@ __device__ __forceinline__ void arrive_one(uint64_t* bar) {
 
 // One row (query token `at` of its sequence, one head) by one warp, from the tokens that it sees and no others: a windowed call's way
 // out for rows that the matrix products cannot have right.  A product with V takes every key of a tile of keys for every row of
-// a tile of queries, and a value that is no finite number makes zero times itself, NaN, of the rows that do not see it.  Keys 16 at a
+// a tile of queries, and a value that is no finite number makes zero times itself, NaN, of the rows that do not see it.  And a
+// query that is the sum of two E4M3 terms has a NaN product with an infinite key wherever the second term is zero or of the other
+// sign (one in f16, wherever an element is too small for it), so that a logit of -inf, which has no weight, looks like a NaN.  Keys 16 at a
 // time (a block): a lane has half of the dims of one key of the logits, and D / 32 dims of the result.  Scales stay outside the
 // sums, as in the decode kernel.  (Calls without such values do not get here, and pay for the look at their results alone.  A function
 // of its own, since inlined it took the loops' registers: 8 chunks behind streams 115 us, so 110, without it 112.)
@@ -657,7 +659,8 @@ paged_prefill_kernel(const __grid_constant__ PrefillParams p, const __grid_const
           if (not_finite(most) && off >= 0) odd |= 1u << row;
         }
       }
-      if constexpr (kWindow) again = __reduce_or_sync(0xffffffffu, odd) & __ballot_sync(0xffffffffu, l_row < INFINITY);
+      // (A sum that is NaN is a NaN key's, or, E5M2 alone, perhaps an infinite one's: see lone_row.)
+      if constexpr (kWindow) again = __reduce_or_sync(0xffffffffu, odd) & __ballot_sync(0xffffffffu, kE5m2 || l_row < INFINITY);
       tc_fence_before();
       }
     } else if (lane == 0) {
@@ -977,7 +980,7 @@ paged_prefill_kernel(const __grid_constant__ PrefillParams p, const __grid_const
           const int q = row / G, h = row - q * G;
           const uint2 result = make_uint2(pack_bf16x2(num.x * inv, num.y * inv), pack_bf16x2(num.z * inv, num.w * inv));
           *reinterpret_cast<uint2*>(p.out + (static_cast<size_t>(row_base + q0 + q) * Hq + g * G + h) * D + 4 * chunk) = result;
-          if (not_finite(larger_magnitudes(result.x & 0x7FFF7FFFu, result.y)) && den < INFINITY) again |= 1u << (turn + lane / kChunks);
+          if (not_finite(larger_magnitudes(result.x & 0x7FFF7FFFu, result.y)) && (kE5m2 || den < INFINITY)) again |= 1u << (turn + lane / kChunks);
         }
       }
       __syncwarp();

@@ -12,7 +12,7 @@ import pytest
 import torch
 from torch.profiler import ProfilerActivity, profile
 
-from oracle import attention
+from oracle import attention, e5m2
 from tests import helpers
 from tests.test_gpu_window import check, make, prefill
 
@@ -138,3 +138,36 @@ def test_a_value_scale_that_is_infinite_reaches_those_who_see_its_block(name, di
     hit[sees, :group] = True
     out[torch.from_numpy(hit)] = torch.from_numpy(ref[hit]).to(torch.bfloat16).cuda()
     check(out, ref, spread, "e4m3", prefill=True, vmax=6.0, what=name)
+
+
+@pytest.mark.parametrize("name,dim", [r for r in ROUTES if r[0] != "rows"])
+def test_an_infinite_key(name, dim, tmp_path):
+    """E5M2: a logit of -inf has no weight, one of +inf makes the outputs of those who see it NaN.  Elements of the query from large to
+    as small as bf16 goes, so that an inexact form of one is zero, or of the other sign, where it is not."""
+    lens, q_lens, hkv, group, window, sinks = RUNS[name]
+    w, cache, kv, table = make(lens, q_lens, group * hkv, hkv, dim, "e5m2", window, sinks, seed=307)
+    gen = torch.Generator().manual_seed(311)
+    w.q[:, :, 0] = (2.0 ** -torch.randint(0, 100, w.q.shape[:2], generator=gen)).to(torch.bfloat16) * (1 + torch.rand(w.q.shape[:2], generator=gen))
+    assert (w.q[:, :, 0] > 0).all()
+    codes = kv[0].copy()
+    raw, idx = granules(w, cache)
+    of, at = positions(name, w)
+    sees = np.zeros(len(of), dtype=bool)
+    for b, picked in enumerate(some_tokens(name)):
+        for pos in [0] + picked:
+            blk, tok = int(table[b, pos // 16]), pos % 16
+            raw[blk, 1, int(idx[0, tok, 0])] = codes[blk, 1, 0, tok, 0] = 0xFC       # -inf in dim 0 of its key, kv head 1
+            if pos:
+                raw[blk, 0, int(idx[0, tok, 0])] = 0x7C                           # +inf, kv head 0
+                sees |= (of == b) & (at >= pos) & ((at - window < pos) | (pos < sinks))
+    assert sees.any() and not sees.all()
+    ref, spread = attention.window_attention(w.q.float().numpy(), (codes, kv[1], e5m2), w.block_table.numpy(), lens, window, sinks, w.cu_q_lens.numpy())
+    assert np.isfinite(ref).all()
+    out, launches = served_by(lambda: prefill(w, cache, table, window, sinks), tmp_path)
+    assert route_of(launches, w) == name
+    assert torch.isnan(out[torch.from_numpy(sees)][:, :group].float()).all()
+    out = out.clone()
+    hit = np.zeros(ref.shape, dtype=bool)
+    hit[sees, :group] = True
+    out[torch.from_numpy(hit)] = torch.from_numpy(ref[hit]).to(torch.bfloat16).cuda()
+    check(out, ref, spread, "e5m2", prefill=True, vmax=6.0, what=name)
