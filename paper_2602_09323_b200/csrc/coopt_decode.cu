@@ -808,6 +808,22 @@ paged_decode_kernel(const __grid_constant__ DecodeParams p, const __grid_constan
       for (int s = 0; s < kQSteps; ++s)
 #pragma unroll
         for (int e = 0; e < 2; ++e) qf[s][e] = pack_f16x2(bf16_lo(qraw[s][e]) * up, bf16_hi(qraw[s][e]) * up);
+      if constexpr (kWindow && C::kE5m2) {
+        // An element below 2^-32 of the row's largest is zero in f16, and zero times an infinite key (E5M2 has them) would be NaN:
+        // windowed calls keep the least f16 of its sign.
+        __half2 least = __half2half2(__ushort_as_half(0x7BFF));
+#pragma unroll
+        for (int s = 0; s < kQSteps; ++s)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) least = __hmin2(least, __habs2(*reinterpret_cast<const __half2*>(&qf[s][e])));
+        const uint32_t bits = *reinterpret_cast<const uint32_t*>(&least);
+        if (row < G && ((bits & 0xFFFFu) == 0u || (bits >> 16) == 0u)) {
+#pragma unroll
+          for (int s = 0; s < kQSteps; ++s)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) qf[s][e] |= __vcmpeq2(qf[s][e] & 0x7FFF7FFFu, 0u) & __vcmpne2(qraw[s][e] & 0x7FFF7FFFu, 0u) & 0x00010001u;
+        }
+      }
       qs[0] = __shfl_sync(0xffffffffu, down, 8 * quad);
       qs[1] = __shfl_sync(0xffffffffu, down, 8 * quad + 4);
     } else {

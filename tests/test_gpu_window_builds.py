@@ -1,0 +1,79 @@
+"""Every build of the windowed decode kernel that a call can be served by: a cluster to a unit (a sequence and kv head), a CTA to a
+unit of which one, two or three fit an SM, and the line.  Which one a call took is read from the device's own record of its
+launches, so that a changed rule on sizes cannot leave one of them untested.  Tolerances: those of tests/test_gpu_window.py."""
+import re
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import attention, e4m3, e5m2
+from paper_2602_09323_b200 import binding
+from tests.test_gpu_window import FMT, check, decode, make
+from tests.test_gpu_window_edges import granules, served_by
+
+pytestmark = pytest.mark.gpu
+
+# name: (sequences, kv heads, window)
+CALLS = {"cluster": (3, 2, 700), "one": (19, 7, 150), "two": (33, 8, 150), "three": (52, 8, 90), "line": (60, 8, 90)}
+SINKS = 9
+BUILDS = [(name, fmt, dim) for name in CALLS for fmt in ("e4m3", "e5m2", "bf16") for dim in (64, 128)]
+
+
+def lengths(name):
+    batch, _, window = CALLS[name]
+    lens = [(b * 7919) % (2 * window) for b in range(batch)]
+    lens[0], lens[1] = 2 * window + 1, 1
+    return lens
+
+
+def route_of(launches, units):
+    """(A bf16 cache takes its new tokens by a launch of its own.)"""
+    (name, grid), = [x for x in launches if "paged_decode_kernel" in x[0]]
+    layers, window, few, runs = re.search(r"paged_decode_kernel<\d+, \d+, (\d+), (\w+), (\d+), (\w+)>", name).groups()
+    assert (layers, window, runs) == ("1", "true", "false"), name
+    if few == "1" and grid > units:
+        return "cluster"
+    return ("line", "one", "two", "three")[int(few)]
+
+
+def problem(name, fmt, dim, seed, poison=True):
+    batch, hkv, window = CALLS[name]
+    lens = lengths(name)
+    w, cache, kv, table = make(lens, [1] * batch, 2 * hkv, hkv, dim, fmt, window, SINKS, seed=seed, poison=poison)
+    return lens, w, cache, kv, table, batch * hkv
+
+
+@pytest.mark.parametrize("name,fmt,dim", BUILDS)
+def test_a_call_against_the_oracle(name, fmt, dim, tmp_path):
+    lens, w, cache, kv, table, units = problem(name, fmt, dim, 401)
+    window = CALLS[name][2]
+    ref, spread = attention.window_attention(w.q.float().numpy(), kv, w.block_table.numpy(), lens, window, SINKS)
+    out, launches = served_by(lambda: decode(w, cache, table, lens, window, SINKS), tmp_path)
+    assert route_of(launches, units) == name
+    check(out, ref, spread, fmt, what=name)
+    assert torch.equal(out, decode(w, cache, table, lens, window, SINKS))
+
+
+@pytest.mark.parametrize("name,dim", [(name, dim) for name in CALLS for dim in (64, 128)])
+def test_a_key_of_minus_infinity_and_queries_from_large_to_small(name, dim, tmp_path):
+    """E5M2: elements of the query as small as bf16 goes do not make a NaN of an infinite key."""
+    lens, w, cache, kv, table, units = problem(name, "e5m2", dim, 409)
+    window = CALLS[name][2]
+    gen = torch.Generator().manual_seed(419)
+    sign = 1 - 2 * torch.randint(0, 2, (w.batch, w.num_kv_heads, 1), generator=gen)
+    w.q[:, :, 0] = ((2.0 ** -torch.randint(0, 133, (w.batch, w.num_kv_heads, 2), generator=gen).double()) * sign).flatten(1).to(torch.bfloat16)
+    assert (w.q[:, :, 0] != 0).all()
+    codes = kv[0].copy()
+    raw, idx = granules(w, cache)
+    for b, L in enumerate(lens):
+        for pos in {0, L - 1} if L > 1 else set():
+            blk = int(table[b, pos // 16])
+            for h in range(w.num_kv_heads):
+                code = 0xFC if sign[b, h] > 0 else 0x7C
+                raw[blk, h, int(idx[0, pos % 16, 0])] = codes[blk, h, 0, pos % 16, 0] = code
+    ref, spread = attention.window_attention(w.q.float().numpy(), (codes, kv[1], e5m2), w.block_table.numpy(), lens, window, SINKS)
+    assert np.isfinite(ref).all()
+    out, launches = served_by(lambda: decode(w, cache, table, lens, window, SINKS), tmp_path)
+    assert route_of(launches, units) == name
+    check(out, ref, spread, "e5m2", what=name)
