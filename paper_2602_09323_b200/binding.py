@@ -180,6 +180,8 @@ class Cache:
             raise CooptError(-2, "coopt_cache_bytes")
         if data is not None and (data.dtype is not torch.uint8 or not data.is_contiguous() or data.numel() != nbytes):
             raise ValueError(f"a cache of this shape is {nbytes} contiguous bytes")
+        if data is not None and not data.is_cuda:
+            raise ValueError("data: memory of a CUDA device (the calls take its address as it is)")
         self.data = torch.zeros(nbytes, dtype=torch.uint8, device=device) if data is None else data
         self.num_blocks, self.num_kv_heads, self.head_dim, self.dtype = num_blocks, num_kv_heads, head_dim, dtype
         self.granule_bytes = lib.coopt_granule_bytes(head_dim, dtype)
