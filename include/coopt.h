@@ -368,6 +368,9 @@ int coopt_window_prefill(const coopt_cache* cache, const void* q, void* out, con
  * coopt_pages_reserve -- row row_ids[i] gets blocks for new_lens[i] tokens: entries without a block between its length and the
  *   new one get one each, refs 1, and its length becomes new_lens[i].  A row is served if the free blocks suffice for it and
  *   the rows before it in the list.  Refused: rows out of range, a row's second mention, lengths that shrink or exceed the table.
+ *   Room and length are one number here, and a windowed release counts back from it: a caller that takes room for more tokens
+ *   than it is about to write sets context_lens back to the tokens written ahead of the next call that reads it (attention, fork,
+ *   release).  Entries past a row's length keep their blocks until the row is released, and reserving again takes what lacks.
  * coopt_pages_fork -- row children[i] becomes a copy of row parents[i]: full blocks are shared (refs + 1), a last block that is
  *   partly filled is copied to a new one in every layer (both may be appended to from then on), released entries stay
  *   released, blocks reserved past the parent's length are not taken over.  Refused: rows out of range, a child whose length is not 0, a

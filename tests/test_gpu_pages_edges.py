@@ -80,3 +80,30 @@ def test_a_fork_with_stale_entries_many_times_over():
             assert np.array_equal(p.pages.context_lens.cpu().numpy(), p.ref.lens), turn
             assert binding.workspace_status(p.ws) == -1
             binding.workspace_init(p.ws)
+
+
+def test_room_taken_ahead_of_what_is_written():
+    """The length set back to the tokens written: a windowed release keeps what the next query sees, a fork shares what is written, and
+    the room stays with its row."""
+    p = Both(60, 8, 12, layers=1, seed=109)
+
+    def reserve_and_set_back(rows, room, written):
+        p.reserve(rows, room)
+        p.pages.context_lens[torch.tensor(rows, device="cuda")] = ints(written)
+        p.ref.lens[rows] = written
+
+    reserve_and_set_back([0, 1], [180, 100], [100, 33])
+    table = p.ref.table.copy()
+    p.release([0, 1], 40, 3)                              # by 180 and 100 tokens the blocks of tokens 48..63, and of 16..47, would go too
+    p.check("windowed release")
+    assert p.ref.table[0].tolist() == [table[0, 0], -1, -1] + table[0, 3:].tolist() and p.ref.table[1].tolist() == table[1].tolist()
+    p.fork([0, 1], [4, 5])
+    p.check("fork")
+    assert p.ref.lens.tolist() == [100, 33, 0, 0, 100, 33, 0, 0] and p.ref.table[5, 3] == -1
+    free = int(np.sum(p.ref.refs == 0))
+    reserve_and_set_back([0, 1, 4], [180, 110, 113], [101, 34, 101])
+    p.check("more of what is there already")
+    assert int(np.sum(p.ref.refs == 0)) == free - 1       # the child's eighth block; the others had theirs
+    p.release([0, 1, 4, 5])
+    p.check("all of it")
+    assert not p.ref.refs.any()
