@@ -7,8 +7,9 @@ import numpy as np
 import pytest
 import torch
 
-from oracle import attention, e4m3, e5m2
-from paper_2602_09323_b200 import binding
+from oracle import attention, e4m3, e5m2, kv_cache
+from paper_2602_09323_b200 import binding, workloads
+from tests import helpers
 from tests.test_gpu_window import FMT, check, decode, make
 from tests.test_gpu_window_edges import granules, served_by
 
@@ -77,3 +78,69 @@ def test_a_key_of_minus_infinity_and_queries_from_large_to_small(name, dim, tmp_
     out, launches = served_by(lambda: decode(w, cache, table, lens, window, SINKS), tmp_path)
     assert route_of(launches, units) == name
     check(out, ref, spread, "e5m2", what=name)
+
+
+@pytest.mark.parametrize("name,fmt,dim", BUILDS)
+def test_new_tokens_in_every_build(name, fmt, dim, tmp_path):
+    """Three steps in a row, so that blocks are opened, their scales grow and stay: the bytes are those of the write rule, the output
+    that of the call over the written cache."""
+    batch, hkv, window = CALLS[name]
+    first = [max(0, L - 3) for L in lengths(name)]
+    first[0] = 2 * window - 2 + (-(2 * window)) % 16       # its third step opens a block
+    w = workloads.make_workload("append", [L + 3 for L in first], 2 * hkv, hkv, dim, seed=421)
+    cache = binding.Cache(w.num_blocks, hkv, dim, FMT[fmt])
+    kind = {"e4m3": e4m3, "e5m2": e5m2}.get(fmt)
+    codes, scales = kv_cache.new_cache(w.num_blocks, hkv, dim)
+    values = kv_cache.new_cache_bf16(w.num_blocks, hkv, dim)
+    rows = np.concatenate([np.arange(w.kv_offsets[b], w.kv_offsets[b] + L) for b, L in enumerate(first)])
+
+    def oracle_write(rows, slots, **more):
+        k, v, slots = w.k[rows].float().numpy(), w.v[rows].float().numpy(), slots.numpy()
+        if fmt == "bf16":
+            kv_cache.kv_write_bf16(values, k, v, slots)
+        else:
+            kv_cache.kv_write(codes, scales, k, v, slots, fmt=kind, **more)
+
+    binding.kv_write(cache, w.k[rows].cuda(), w.v[rows].cuda(), w.slot_mapping[rows].cuda())
+    oracle_write(rows, w.slot_mapping[rows])
+    ws = binding.new_workspace(batch, 2 * hkv, hkv, dim, w.block_table.shape[1])
+    table, gen = w.block_table.cuda(), torch.Generator().manual_seed(431)
+    for step in range(3):
+        lens = [L + step + 1 for L in first]
+        lens[2] = 0                                        # a row of the batch without a sequence
+        last = torch.tensor([w.kv_offsets[b] + first[b] + step for b in range(batch)])
+        slots = w.slot_mapping[last].clone()
+        slots[2] = -1
+        oracle_write(last.numpy(), slots, **({} if fmt == "bf16" else {"reciprocal": True}))
+        q = torch.randn(batch, 2 * hkv, dim, generator=gen).to(torch.bfloat16).cuda()
+        args = (cache, q, table, torch.tensor(lens, dtype=torch.int32).cuda(), window, SINKS, w.sm_scale, ws)
+        new = (w.k[last].cuda(), w.v[last].cuda(), slots.cuda())
+        out, launches = served_by(lambda: binding.window_decode(*args, *new), tmp_path)
+        assert route_of(launches, batch * hkv) == name
+        want = binding.window_decode(*args)
+        torch.cuda.synchronize()
+        assert binding.workspace_status(ws) == 0
+        if fmt == "bf16":
+            assert np.array_equal(helpers.cache_to_logical(cache), values), step
+        else:
+            helpers.check_cache_bit_exact(cache, codes, scales, what=f"step {step}")
+        assert torch.equal(out, want) and torch.all(out[2] == 0), step
+
+
+@pytest.mark.parametrize("name,fmt,dim", BUILDS)
+def test_a_nan_key_in_every_build(name, fmt, dim, tmp_path):
+    """The last token's key of kv head 0: its outputs are NaN, all others as they were."""
+    lens, w, cache, kv, table, units = problem(name, fmt, dim, 433)
+    window = CALLS[name][2]
+    before = decode(w, cache, table, lens, window, SINKS)
+    there = torch.tensor([L > 0 for L in lens])
+    raw, idx = granules(w, cache)
+    for b, L in enumerate(lens):
+        if L:
+            at = int(idx[0, (L - 1) % 16, dim - 1])
+            for byte in range(2 if fmt == "bf16" else 1):
+                raw[int(table[b, (L - 1) // 16]), 0, at + byte] = 0xC0 if fmt == "bf16" and byte == 0 else 0x7F
+    out, launches = served_by(lambda: decode(w, cache, table, lens, window, SINKS), tmp_path)
+    assert route_of(launches, units) == name
+    assert torch.isnan(out[there][:, :2].float()).all()
+    assert torch.equal(out[:, 2:], before[:, 2:]) and torch.equal(out[~there], before[~there])

@@ -33,7 +33,7 @@ ROUTES = [(name, dim) for name, dims in KERNELS.items() for dim in dims]
 
 def served_by(call, tmp_path):
     """The result of a call, and which kernel gave it."""
-    with profile(activities=[ProfilerActivity.CUDA]) as prof:
+    with profile(activities=[ProfilerActivity.CUDA], acc_events=True) as prof:
         result = call()
         torch.cuda.synchronize()
     path = str(tmp_path / "launches.json")
@@ -171,3 +171,26 @@ def test_an_infinite_key(name, dim, tmp_path):
     hit[sees, :group] = True
     out[torch.from_numpy(hit)] = torch.from_numpy(ref[hit]).to(torch.bfloat16).cuda()
     check(out, ref, spread, "e5m2", prefill=True, vmax=6.0, what=name)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("name,dim", ROUTES)
+def test_a_nan_key_reaches_those_who_see_it_and_no_one_else(name, dim, fmt, tmp_path):
+    """Keys that only a part of a run sees, of kv head 1."""
+    w, cache, table, ref, spread = runs(name, dim, fmt, seed=313)
+    group, window, sinks = RUNS[name][3:]
+    raw, idx = granules(w, cache)
+    of, at = positions(name, w)
+    before = prefill(w, cache, table, window, sinks)
+    check(before, ref, spread, fmt, prefill=True, vmax=6.0, what=name)
+    sees = np.zeros(len(of), dtype=bool)
+    for b, picked in enumerate(some_tokens(name)):
+        for pos in picked:
+            raw[int(table[b, pos // 16]), 1, int(idx[0, pos % 16, 3])] = 0x7F
+            sees |= (of == b) & (at >= pos) & ((at - window < pos) | (pos < sinks))
+    assert sees.any() and not sees.all()
+    out, launches = served_by(lambda: prefill(w, cache, table, window, sinks), tmp_path)
+    assert route_of(launches, w) == name
+    sees = torch.from_numpy(sees)
+    assert torch.isnan(out[sees][:, group:2 * group].float()).all()
+    assert torch.equal(out[~sees], before[~sees]) and torch.equal(out[:, :group], before[:, :group]) and torch.equal(out[:, 2 * group:], before[:, 2 * group:])
