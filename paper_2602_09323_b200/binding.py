@@ -484,6 +484,8 @@ def window_decode(cache: Cache, q: torch.Tensor, block_table: torch.Tensor, cont
                              "on the current CUDA device")
         stride = at[0] if rows > 1 else heads * dim
         k, v, slots = k_new.data_ptr(), v_new.data_ptr(), slot_mapping.data_ptr()
+    if shape[0] == 0:                      # (no tensor without elements has an address)
+        return out
     st = (_lib or load_library()).coopt_window_decode(cache._ref, k, v, stride, slots, q.data_ptr(), out.data_ptr(), block_table.data_ptr(), width[1],
                                             context_lens.data_ptr(), shape[0], shape[1], _int32(window), _int32(sinks), float(sm_scale), workspace.data_ptr(),
                                             workspace.numel(), _stream_of(device))
@@ -507,6 +509,8 @@ def window_prefill(cache: Cache, q: torch.Tensor, cu_q_lens: torch.Tensor, block
         _window_inputs(cache, q, block_table, context_lens, workspace, out, None)
     if not (cu_q_lens.dtype is _I32 and cu_q_lens.is_contiguous() and cu_q_lens.numel() == width[0] + 1 and cu_q_lens.get_device() == device):
         raise ValueError("cu_q_lens: contiguous int32 [B + 1] on the current CUDA device")
+    if shape[0] == 0:                      # (no tensor without elements has an address)
+        return out
     st = (_lib or load_library()).coopt_window_prefill(cache._ref, q.data_ptr(), out.data_ptr(), cu_q_lens.data_ptr(), block_table.data_ptr(), width[1],
                                              context_lens.data_ptr(), width[0], shape[1], shape[0], _int32(window), _int32(sinks), float(sm_scale),
                                              workspace.data_ptr(), workspace.numel(), _stream_of(device))

@@ -13,6 +13,7 @@ import torch
 from torch.profiler import ProfilerActivity, profile
 
 from oracle import attention, e5m2
+from paper_2602_09323_b200 import binding
 from tests import helpers
 from tests.test_gpu_window import check, make, prefill
 
@@ -194,3 +195,24 @@ def test_a_nan_key_reaches_those_who_see_it_and_no_one_else(name, dim, fmt, tmp_
     sees = torch.from_numpy(sees)
     assert torch.isnan(out[sees][:, group:2 * group].float()).all()
     assert torch.equal(out[~sees], before[~sees]) and torch.equal(out[:, :group], before[:, :group]) and torch.equal(out[:, 2 * group:], before[:, 2 * group:])
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "bf16"])
+def test_calls_without_a_query(fmt):
+    """A step in which no sequence takes part, and a batch of runs that are all empty."""
+    w, cache, kv, table = make([40, 70], [1, 1], 4, 2, 64, fmt, 9, 1, seed=317)
+    ws = binding.new_workspace(2, 4, 2, 64, table.shape[1])
+    q, none = torch.zeros(0, 4, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(0, dtype=torch.int32, device="cuda")
+    new = torch.zeros(0, 2, 64, dtype=torch.bfloat16, device="cuda")
+    before = cache.data.clone()
+    for more in ((), (new, new, none.long())):
+        out = binding.window_decode(cache, q, table[:0].cuda(), none, 9, 1, w.sm_scale, ws, *more)
+        assert out.shape == q.shape
+    if fmt != "bf16":
+        out = binding.window_prefill(cache, q, torch.zeros(3, dtype=torch.int32, device="cuda"), table.cuda(), torch.tensor([40, 70], dtype=torch.int32, device="cuda"),
+                                     9, 1, w.sm_scale, ws)
+        assert out.shape == q.shape
+        with pytest.raises(ValueError):
+            binding.window_prefill(cache, q, torch.zeros(2, dtype=torch.int32, device="cuda"), table.cuda(), none, 9, 1, w.sm_scale, ws)
+    torch.cuda.synchronize()
+    assert binding.workspace_status(ws) == 0 and torch.equal(cache.data, before)
