@@ -317,7 +317,8 @@ int coopt_decode_step_host(const coopt_cache* cache, const void* step_inputs_hos
  * Softmax, scales and grouping are those of coopt_paged_decode.  Only blocks that hold a visible token of some query of the
  * sequence are read, and only their table entries: what lies between the sinks and the window may have been released
  * (coopt_pages_release) and hold any entry.  A window that reaches back to the sequence's start gives coopt_paged_decode's
- * (coopt_paged_chunked's causal) result.
+ * (coopt_paged_chunked's causal) result, as long as what it sees is finite (those calls leave a NaN out where pieces of a
+ * softmax are joined; these do as follows).
  *   window >= 1, sinks >= 0; either may exceed the contexts.
  * A key that is NaN makes the outputs of the queries that see it NaN, and of no others; one whose logit is -inf has no weight.
  * A value that is not finite reaches, in its dim, the outputs of the queries that see its token, and of no others (a scale that is
@@ -327,8 +328,9 @@ int coopt_decode_step_host(const coopt_cache* cache, const void* step_inputs_hos
  *   k_new, v_new, slot_mapping  the step's new tokens, written first, as for coopt_decode_step_planned (the same precondition:
  *                               the new token of sequence b is its last position).  FP8 caches take them in the same launch, by
  *                               coopt_kv_write's rule but for the rounding of the scale: amax times the fp32 reciprocal of 448
- *                               (57344), at most one unit in the last place from amax / 448.  A bf16 cache takes them in a
- *                               launch of its own.  All three NULL = none
+ *                               (57344), at most one unit in the last place from amax / 448.  A caller whose caches have to
+ *                               be the same bytes whichever call wrote a token writes it with coopt_kv_write and passes none
+ *                               here.  A bf16 cache takes them in a launch of its own.  All three NULL = none
  *   context_lens                counting the new token; 0 gives an all-zero output row
  * coopt_window_prefill -- runs of query tokens; the arguments of coopt_paged_chunked without chunks, always causal.
  *   cu_q_lens                   runs may have any length, 0 and 1 included; total_q = cu_q_lens[batch] sizes the launch, and rows

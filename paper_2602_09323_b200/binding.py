@@ -462,7 +462,8 @@ def window_decode(cache: Cache, q: torch.Tensor, block_table: torch.Tensor, cont
                   sm_scale: float, workspace: torch.Tensor, k_new: Optional[torch.Tensor] = None, v_new: Optional[torch.Tensor] = None,
                   slot_mapping: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """coopt_window_decode: q bf16 [B, Hq, D] sees the last ``window`` tokens and the first ``sinks``; with k_new, v_new
-    (bf16 [B, Hkv, D], token stride taken from the tensor) and slot_mapping (int64 [B]) the new tokens are written first."""
+    (bf16 [B, Hkv, D], token stride taken from the tensor) and slot_mapping (int64 [B]) the new tokens are written first (FP8:
+    with a block scale that may be an ulp from kv_write's; write them with kv_write where the bytes have to be the same)."""
     if out is None:
         out = torch.empty_like(q)
     device, shape, width = _device(), q.shape, block_table.shape
@@ -591,7 +592,8 @@ def pages_copy(caches: CacheSet, src: torch.Tensor, dst: torch.Tensor) -> None:
 
 
 def pages_reserve(pages: Pages, row_ids: torch.Tensor, new_lens: torch.Tensor, workspace: torch.Tensor) -> None:
-    """coopt_pages_reserve: row row_ids[i] gets blocks for new_lens[i] tokens, which becomes its length."""
+    """coopt_pages_reserve: row row_ids[i] gets blocks for new_lens[i] tokens, which becomes its length (set pages.context_lens back
+    where that is room ahead of what is written: attention, fork and release read it)."""
     device = _device()
     n = _lists(device, row_ids, new_lens)
     _pool_here(device, pages, workspace)
@@ -601,7 +603,7 @@ def pages_reserve(pages: Pages, row_ids: torch.Tensor, new_lens: torch.Tensor, w
 
 
 def pages_fork(caches: CacheSet, pages: Pages, parents: torch.Tensor, children: torch.Tensor, workspace: torch.Tensor) -> None:
-    """coopt_pages_fork: row children[i] becomes a copy of row parents[i] that shares its full blocks."""
+    """coopt_pages_fork: row children[i] becomes a copy of row parents[i] that shares its full blocks (those in use)."""
     device = _device()
     n = _lists(device, parents, children)
     _pool_here(device, pages, workspace, caches)

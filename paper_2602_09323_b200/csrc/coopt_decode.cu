@@ -196,11 +196,12 @@ template <bool kE5m2> __device__ __forceinline__ uint32_t codes_lo(uint32_t w) {
 template <bool kE5m2> __device__ __forceinline__ uint32_t codes_hi(uint32_t w) { return kE5m2 ? e5m2x2_to_f16x2_hi(w) : e4m3x2_to_f16x2_hi(w); }
 
 // Algorithm 1 phase 1 for one token, on the granule as it sits in shared memory (K part, V part, header), which is then
-// written back: the write kernels' rule (write_part), with the same value for every number that is stored.
-// k, v: this lane's D / 32 consecutive values of the token's rows, as packed pairs.
+// written back.  k, v: this lane's D / 32 consecutive values of the token's rows, as packed pairs.
+// Without kReciprocal this is the write kernels' rule (write_part), with the same value for every number that is stored.
 // kReciprocal (windowed calls): the scale of the token's largest magnitude is that times the rounded reciprocal of the format's
-// largest value, and not the quotient, from which it differs by one unit in the last place at most.  The codes follow from
-// the scale by the same rule (a value that then lies beyond the largest code by a rounding takes that code).
+// largest value, and not the quotient, from which it differs by one unit in the last place at most: one rounding more, and
+// bytes that may differ from the other writes' of the same token.  The codes follow from the scale by the same rule (a value
+// that then lies beyond the largest code by a rounding takes that code).
 template <int D, bool kE5m2, bool kReciprocal>
 __device__ __noinline__ void append_token(uint8_t* st, uint8_t* gran, const uint2 k, const uint2 v, int off, int lane) {
   constexpr int kPart = kBlockSize * D, kPerLane = D / 32;

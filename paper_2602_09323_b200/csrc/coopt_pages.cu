@@ -80,7 +80,7 @@ __device__ __forceinline__ int cta_scan(int x, int* warp_sums, int& total) {
   return before + inc - x;
 }
 struct Slice {
-  unsigned* bits;          // shared memory: bit set = used; past the end of the pool: set, and not counted
+  unsigned* bits;          // shared memory: bit set = used; past the end of the pool: clear, and not taken for free (write_free)
   int first, words, per_thread;
   int before;              // used blocks of the slices before, then (thread) of the words before
   int used;                // .. of the whole pool
