@@ -166,8 +166,9 @@ __device__ __forceinline__ void arrive_one(uint64_t* bar) {
 // query that is the sum of two E4M3 terms has a NaN product with an infinite key wherever the second term is zero or of the other
 // sign (one in f16, wherever an element is too small for it), so that a logit of -inf, which has no weight, looks like a NaN.  Keys 16 at a
 // time (a block): a lane has half of the dims of one key of the logits, and D / 32 dims of the result.  Scales stay outside the
-// sums, as in the decode kernel.  (Calls without such values do not get here, and pay for the look at their results alone.  A function
-// of its own, since inlined it took the loops' registers: 8 chunks behind streams 115 us, so 110, without it 112.)
+// sums, as in the decode kernel.  It is a way to be right, not fast: 8 chunks behind streams, window 1024, with a NaN value of one kv
+// head in each that half of the run sees take 5.4 ms.  Calls without such values do not get here, and pay for the look at their results
+// alone.  (A function of its own, since inlined it took the loops' registers: the 8 chunks 115 us, so 110, without it 112.)
 template <int D, bool kE5m2>
 __device__ __noinline__ void lone_row(const PrefillParams& p, int b, int g, size_t row, int at, int lane) {
   constexpr int kPer = D / 32;
@@ -185,14 +186,20 @@ __device__ __noinline__ void lone_row(const PrefillParams& p, int b, int g, size
     if (id < 0 || id >= p.num_blocks) id = 0;          // (reported where it was first looked at)
     const uint8_t* gran = p.cache + (static_cast<size_t>(id) * p.num_kv_heads + g) * granule_bytes(D, true);
     const float2 scale = *reinterpret_cast<const float2*>(gran + header_offset(D));
+    uint4 k[kPer], vs[kPer];                           // (all on their way at once)
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int d = lane * kPer + i;
+      k[i] = *reinterpret_cast<const uint4*>(gran + (tok >> 3) * 8 * D + (c0 + i) * 128 + (tok & 7) * 16);
+      vs[i] = *reinterpret_cast<const uint4*>(gran + kBlockSize * D + (d >> 3) * 128 + (d & 7) * 16);
+    }
     float dot = 0.0f;
-#pragma unroll 1
-    for (int c = c0; c < c0 + kPer; ++c) {
-      const uint4 k = *reinterpret_cast<const uint4*>(gran + (tok >> 3) * 8 * D + c * 128 + (tok & 7) * 16);
-      const uint32_t w[4] = {k.x, k.y, k.z, k.w};
+#pragma unroll
+    for (int c = 0; c < kPer; ++c) {
+      const uint32_t w[4] = {k[c].x, k[c].y, k[c].z, k[c].w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const uint2 h = widen4<kE5m2>(w[i]), qv = *reinterpret_cast<const uint2*>(q + 16 * c + 4 * i);
+        const uint2 h = widen4<kE5m2>(w[i]), qv = *reinterpret_cast<const uint2*>(q + 16 * (c0 + c) + 4 * i);
         const float2 lo = f16x2_to_f32(h.x), hi = f16x2_to_f32(h.y);
         dot += bf16_lo(qv.x) * lo.x + bf16_hi(qv.x) * lo.y + bf16_lo(qv.y) * hi.x + bf16_hi(qv.y) * hi.y;
       }
@@ -212,17 +219,17 @@ __device__ __noinline__ void lone_row(const PrefillParams& p, int b, int g, size
     const unsigned seen = __ballot_sync(0xffffffffu, sees);
 #pragma unroll
     for (int t4 = 0; t4 < 4; ++t4) {
+      float wt[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) wt[t] = __shfl_sync(0xffffffffu, w, 4 * t4 + t);
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
-        const int d = lane * kPer + i;
-        const uint2 h = widen4<kE5m2>(*reinterpret_cast<const uint32_t*>(gran + kBlockSize * D + (d >> 3) * 128 + (d & 7) * 16 + 4 * t4));
+        const uint2 h = widen4<kE5m2>(t4 == 0 ? vs[i].x : t4 == 1 ? vs[i].y : t4 == 2 ? vs[i].z : vs[i].w);
         const float2 lo = f16x2_to_f32(h.x), hi = f16x2_to_f32(h.y);
         const float e[4] = {lo.x, lo.y, hi.x, hi.y};
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const float wt = __shfl_sync(0xffffffffu, w, 4 * t4 + t);
-          if ((seen >> (4 * t4 + t)) & 1u) v[i] += wt * e[t];
-        }
+        for (int t = 0; t < 4; ++t)
+          if ((seen >> (4 * t4 + t)) & 1u) v[i] += wt[t] * e[t];
       }
     }
 #pragma unroll
