@@ -261,8 +261,8 @@ struct Acc {
 };
 __device__ __forceinline__ void acc_clear(Acc& a) { a.M = -INFINITY; a.den = 0.0f; a.num = make_float4(0.0f, 0.0f, 0.0f, 0.0f); }
 // Up to 32 more pieces into the accumulator.  Lane k brings piece k's maximum and sum; `rows(k)` is where the piece's o
-// (normalised by its sum) lies for this lane.  kNan: a piece whose sum is NaN (a key that is seen was) makes the result NaN; else
-// it is left out.
+// (normalised by its sum) lies for this lane.  kNan: a piece whose sum is NaN (a key that is seen was) makes the result NaN, and so
+// does one whose o is, even where its weight is zero in fp32; else they are left out.
 template <bool kGlobal, bool kNan, class Rows>
 __device__ __forceinline__ void acc_merge(Acc& a, int n, float m, float l, bool on, Rows rows) {
   constexpr int kUnroll = 4;
@@ -276,6 +276,7 @@ __device__ __forceinline__ void acc_merge(Acc& a, int n, float m, float l, bool 
   };
   fetch(0);                              // (on their way while the weights are worked out)
   const bool some = kNan ? !(l <= 0.0f) : l > 0.0f;
+  [[maybe_unused]] const unsigned held = kNan ? __ballot_sync(0xffffffffu, some) : 0u;
   const float top = fmaxf(a.M, ordered_to_f32(__reduce_max_sync(0xffffffffu, f32_to_ordered(some ? m : -INFINITY))));
   const float wgt = some ? l * ex2(m - top) : 0.0f;
   const float keep = a.den > 0.0f ? ex2(a.M - top) : 0.0f;
@@ -287,7 +288,7 @@ __device__ __forceinline__ void acc_merge(Acc& a, int n, float m, float l, bool 
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k) {
       const float w = k0 + k < n ? __shfl_sync(0xffffffffu, wgt, k0 + k) : 0.0f;
-      if (kNan ? !(w <= 0.0f) : w > 0.0f) { a.num.x += w * o[k].x; a.num.y += w * o[k].y; a.num.z += w * o[k].z; a.num.w += w * o[k].w; }
+      if (kNan ? ((held >> (k0 + k)) & 1u) != 0u : w > 0.0f) { a.num.x += w * o[k].x; a.num.y += w * o[k].y; a.num.z += w * o[k].z; a.num.w += w * o[k].w; }
     }
     k0 += kUnroll;
     if (k0 >= n) break;

@@ -144,3 +144,27 @@ def test_a_nan_key_in_every_build(name, fmt, dim, tmp_path):
     assert route_of(launches, units) == name
     assert torch.isnan(out[there][:, :2].float()).all()
     assert torch.equal(out[:, 2:], before[:, 2:]) and torch.equal(out[~there], before[~there])
+
+
+@pytest.mark.parametrize("name,fmt,dim", BUILDS)
+def test_a_nan_value_without_weight_in_every_build(name, fmt, dim, tmp_path):
+    """Logits so far apart that nearly all weights, and those of whole pieces of a softmax, are zero in fp32: zero times NaN is NaN
+    wherever the token lies.  The other dims are as they were."""
+    lens, w, cache, kv, table, units = problem(name, fmt, dim, 439)
+    window = CALLS[name][2]
+    w.q *= 512
+    before = decode(w, cache, table, lens, window, SINKS)
+    raw, idx = granules(w, cache)
+    there = torch.tensor([L > 0 for L in lens])
+    for b, L in enumerate(lens):
+        if L:
+            for h in range(w.num_kv_heads):
+                pos = L - 1 - (37 * b + 11 * h) % min(L, window)
+                at = int(idx[1, pos % 16, 5])
+                for byte in range(2 if fmt == "bf16" else 1):
+                    raw[int(table[b, pos // 16]), h, at + byte] = 0xC0 if fmt == "bf16" and byte == 0 else 0x7F
+    out, launches = served_by(lambda: decode(w, cache, table, lens, window, SINKS), tmp_path)
+    assert route_of(launches, units) == name
+    assert torch.isnan(out[there][:, :, 5].float()).all()
+    rest = [d for d in range(dim) if d != 5]
+    assert torch.equal(out[there][:, :, rest], before[there][:, :, rest]) and torch.equal(out[~there], before[~there])
