@@ -610,7 +610,9 @@ paged_prefill_kernel(const __grid_constant__ PrefillParams p, const __grid_const
     ok = __all_sync(0xffffffffu, ok);
     if (ok) {
       tc_fence_after();
-      const float k = (kWindow ? !(l_row <= 0.0f) : l_row > 0.0f) ? v_ref / l_row : 0.0f;      // (kWindow: a NaN sum makes the row NaN)
+      // (kWindow: a NaN sum makes the row NaN, and a NaN value does so under scales that are all zero, too)
+      const float k = (kWindow ? !(l_row <= 0.0f) : l_row > 0.0f) ? v_ref / l_row : 0.0f;
+      const bool some = kWindow ? !(l_row <= 0.0f) : k != 0.0f;
       // The rows go through shared memory, where the tile's query operand was (its products are done): 16 bytes of a row at
       // (chunk ^ row).
       if constexpr (kSplit) {
@@ -628,7 +630,7 @@ paged_prefill_kernel(const __grid_constant__ PrefillParams p, const __grid_const
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-              auto f = [&](int e) { return k != 0.0f ? __uint_as_float(o[4 * j + e]) * k : 0.0f; };
+              auto f = [&](int e) { return some ? __uint_as_float(o[4 * j + e]) * k : 0.0f; };
               *reinterpret_cast<float4*>(part + ((8 * c + j) ^ (r & (kChunks - 1))) * 4) = make_float4(f(0), f(1), f(2), f(3));
             }
           }
@@ -649,7 +651,7 @@ paged_prefill_kernel(const __grid_constant__ PrefillParams p, const __grid_const
         }
         uint32_t w[16];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) w[j] = k != 0.0f ? pack_bf16x2(__uint_as_float(o[2 * j]) * k, __uint_as_float(o[2 * j + 1]) * k) : 0u;
+        for (int j = 0; j < 16; ++j) w[j] = some ? pack_bf16x2(__uint_as_float(o[2 * j]) * k, __uint_as_float(o[2 * j + 1]) * k) : 0u;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
           *reinterpret_cast<uint4*>(rows + lane * D * 2 + ((4 * c + j) ^ (lane & (kLanes - 1))) * 16) = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);

@@ -225,3 +225,30 @@ def test_calls_without_a_query(fmt):
             binding.window_prefill(cache, q, torch.zeros(2, dtype=torch.int32, device="cuda"), table.cuda(), none, 9, 1, w.sm_scale, ws)
     torch.cuda.synchronize()
     assert binding.workspace_status(ws) == 0 and torch.equal(cache.data, before)
+
+
+@pytest.mark.parametrize("name,dim", ROUTES)
+def test_a_nan_value_under_scales_that_are_zero(name, dim, tmp_path):
+    """What a token leaves whose value is NaN where its block holds zeros: NaN codes under a scale of zero."""
+    w, cache, table, ref, spread = runs(name, dim, "e4m3", seed=331)
+    lens, q_lens, _, group, window, sinks = RUNS[name]
+    raw, idx = granules(w, cache)
+    raw[:, 0, 16 * dim:32 * dim] = 0
+    raw[:, 0, 32 * dim + 4:32 * dim + 8] = 0
+    ref[:, :group], spread[:, :group] = 0, 0
+    of, at = positions(name, w)
+    sees = np.zeros(len(of), dtype=bool)
+    for b, picked in enumerate(some_tokens(name)):
+        for pos in picked:
+            raw[int(table[b, pos // 16]), 0, int(idx[1, pos % 16, 7])] = 0x7F
+            sees |= (of == b) & (at >= pos) & ((at - window < pos) | (pos < sinks))
+    assert sees.any() and not sees.all()
+    out, launches = served_by(lambda: prefill(w, cache, table, window, sinks), tmp_path)
+    check_route(launches, w, name)
+    out = out.clone()
+    hit = np.zeros(ref.shape, dtype=bool)
+    hit[sees, :group, 7] = True
+    assert torch.isnan(out[torch.from_numpy(hit)].float()).all()
+    out[torch.from_numpy(hit)] = 0
+    assert not out[:, :group].any()
+    check(out, ref, spread, "e4m3", prefill=True, vmax=6.0, what=name)
